@@ -45,7 +45,8 @@ typedef enum {
   MOE_ERR_DTYPE = -3,     /* unsupported (in_dtype, out_dtype) pair                  */
   MOE_ERR_ALIGN = -4,     /* a device pointer is not 16-byte aligned                 */
   MOE_ERR_WORKSPACE = -5, /* workspace_bytes smaller than moe_workspace_bytes(cfg)   */
-  MOE_ERR_HIP = -6        /* a HIP runtime call (launch, event record) failed        */
+  MOE_ERR_HIP = -6,       /* a HIP runtime call (launch, event record) failed        */
+  MOE_ERR_OVERLAP = -7    /* memory that the call would write is named twice         */
 } moe_status;
 
 typedef enum { MOE_F32 = 0, MOE_BF16 = 1, MOE_F16 = 2 } moe_dtype;
@@ -335,6 +336,61 @@ int moe_layer_forward_aux(const moe_config* cfg, const void* x, const void* Wg, 
                           const void* W1, const void* W2, void* out, float* l_aux, float* mean_prob,
                           int32_t* first_counts, void* workspace, size_t workspace_bytes,
                           void* const* stage_events, void* stream);
+
+/* Optimizer step (Section 4.1: Adam with float32 master weights and moments): AdamW over many tensors, one launch.
+ * With g = grad * grad_scale, t the step and per tensor lr = values.lr * lr_scale:
+ *   m' = beta1 m + (1 - beta1) g                 v' = beta2 v + (1 - beta2) g^2
+ *   p' = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)
+ *   half = p' rounded to nearest even
+ * in float32, in this order (the factors of t and lr in float64, rounded once).  p, g: float32 [n].
+ * moment_bits 32: m, v float32 [n].
+ * moment_bits 8: 32 consecutive elements share one power of two (uint8: 2^(power - 127), the e8m0 format), each is one
+ * e4m3 code; m holds m, v holds sqrt(v).  power = the least of at least 27 that keeps the block's largest value at most 448 codes
+ * units.  A value is rounded down to a code, or up when the part of the code step above it plus a phase is at
+ * least 1; the phase is ((i mod 512) * 0x85EBCA6B + t * 0x9E3779B9 mod 2^32) / 2^32 cut to 20 bits for element i of a tensor's m,
+ * and half a turn from it for v: over the steps the mean is right, as rounding to nearest, which would hold v still, is
+ * not.  A positive root gets at least the smallest code.  A block with an infinite or NaN value becomes NaN (power 255, codes
+ * 127).  Zeros (codes and powers) are the moments before the first step.
+ *
+ * moe_adamw_plan checks the tensors (HOST array; the pointers in it are device pointers, 16-byte aligned; m_power
+ * and v_power only with moment_bits 8; half may be NULL; n == 0 is allowed) and fills `plan` (HOST memory of at least
+ * moe_adamw_plan_bytes bytes, 0 on invalid arguments) and *n_chunks.  The caller copies the plan to device memory once and
+ * keeps it as long as the tensors stay where they are.  Memory that would be written by two tensors, or twice by one, or is the gradient of
+ * one and written by another is refused (MOE_ERR_OVERLAP).
+ * moe_adamw_step makes the step: plan and values in DEVICE memory, n_tensors and n_chunks as in the plan.  The values are read by the kernel,
+ * so a captured call replays with what they hold then.  skip != 0: nothing is written (a program that
+ * found its gradients infinite).  step counts from 1 (less is taken as 1).  Every element is written by one thread: the
+ * same bits on every run.  0 <= beta < 1, eps > 0 as a float32. */
+typedef struct {
+  double beta1, beta2, eps;
+  int32_t moment_bits;      /* 32 or 8 */
+  int32_t reserved;
+} moe_adamw_config;
+typedef struct {
+  float* p;
+  const float* g;
+  void* m;
+  void* v;
+  uint8_t* m_power;         /* [ceil(n / 32)] */
+  uint8_t* v_power;
+  void* half;               /* [n] of half_dtype, or NULL */
+  int64_t n;
+  int32_t half_dtype;       /* MOE_BF16 or MOE_F16 */
+  float lr_scale;
+  float weight_decay;
+  int32_t reserved;
+} moe_adamw_tensor;
+typedef struct {
+  int32_t step;
+  int32_t skip;
+  float lr;
+  float grad_scale;
+} moe_adamw_values;
+size_t moe_adamw_plan_bytes(const moe_adamw_config* cfg, const moe_adamw_tensor* tensors, int32_t n_tensors);
+int moe_adamw_plan(const moe_adamw_config* cfg, const moe_adamw_tensor* tensors, int32_t n_tensors, void* plan,
+                   size_t plan_bytes, int64_t* n_chunks);
+int moe_adamw_step(const moe_adamw_config* cfg, const void* plan, int32_t n_tensors, int64_t n_chunks,
+                   const moe_adamw_values* values, void* stream);
 
 /* Which stages moe_layer_forward folds into the expert GEMMs for `cfg` (bf16 / fp16 input; neither if d is
  * no multiple of 64 and below 456, nor the combine if F is, except on the few rows of token generation): a mask of

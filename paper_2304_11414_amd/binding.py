@@ -28,6 +28,16 @@ class MoeWorkspaceLayout(Structure):
                                         "logits", "aux")]
 
 
+class MoeAdamwConfig(Structure):
+    _fields_ = [("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("moment_bits", c_int32),
+                ("reserved", c_int32)]
+
+
+class MoeAdamwTensor(Structure):
+    _fields_ = [(n, c_void_p) for n in ("p", "g", "m", "v", "m_power", "v_power", "half")] + [
+        ("n", c_int64), ("half_dtype", c_int32), ("lr_scale", c_float), ("weight_decay", c_float), ("reserved", c_int32)]
+
+
 class MoeError(RuntimeError):
     pass
 
@@ -66,6 +76,10 @@ _PROTOTYPES = {
     "moe_layer_forward": (c_int, [POINTER(MoeConfig)] + [c_void_p] * 7 + [c_size_t, POINTER(c_void_p), c_void_p]),
     "moe_layer_forward_aux": (c_int, [POINTER(MoeConfig)] + [c_void_p] * 10 + [c_size_t, POINTER(c_void_p), c_void_p]),
     "moe_layer_fuses": (c_int, [POINTER(MoeConfig)]),
+    "moe_adamw_plan_bytes": (c_size_t, [POINTER(MoeAdamwConfig), POINTER(MoeAdamwTensor), c_int32]),
+    "moe_adamw_plan": (c_int, [POINTER(MoeAdamwConfig), POINTER(MoeAdamwTensor), c_int32, c_void_p, c_size_t,
+                               POINTER(c_int64)]),
+    "moe_adamw_step": (c_int, [POINTER(MoeAdamwConfig), c_void_p, c_int32, c_int64, c_void_p, c_void_p]),
     "moe_copy_bytes": (c_int, [c_void_p, c_void_p, c_size_t, c_void_p]),
     "moe_mfma_probe": (c_int, [c_int64, c_int, c_void_p, POINTER(c_double), c_void_p]),
     "moe_event_create": (c_int, [POINTER(c_void_p)]),
@@ -326,6 +340,69 @@ MOE_FUSE_SLICE, MOE_FUSE_COMBINE = 1, 2
 def moe_layer_fuses(cfg) -> int:
     """Mask of MOE_FUSE_SLICE / MOE_FUSE_COMBINE: the stages moe_layer_forward folds into the GEMMs."""
     return load_library().moe_layer_fuses(byref(cfg))
+
+
+def make_adamw_config(beta1=0.9, beta2=0.999, eps=1e-8, moment_bits=32) -> MoeAdamwConfig:
+    return MoeAdamwConfig(float(beta1), float(beta2), float(eps), int(moment_bits), 0)
+
+
+class AdamwPlan:
+    """The tensors of a step: the plan in device memory, and the tensors it points into (kept alive)."""
+
+    def __init__(self, memory, n_tensors, n_chunks, tensors):
+        self.memory, self.n_tensors, self.n_chunks, self.tensors = memory, n_tensors, n_chunks, tensors
+
+
+def moe_adamw_plan(cfg, tensors) -> AdamwPlan:
+    """`tensors`: a list of dicts of contiguous device tensors p, g (float32), m, v (float32, or uint8 with 8-bit moments, then
+    m_power and v_power as well), half (bfloat16 or float16, may be missing), and numbers lr_scale (1), weight_decay (0)."""
+    import torch
+    moment = torch.uint8 if cfg.moment_bits == 8 else torch.float32
+    table = (MoeAdamwTensor * max(len(tensors), 1))()
+    device = None
+    for entry, t in zip(table, tensors):
+        n = t["p"].numel()
+        powers = (n + 31) // 32
+        wanted = {"p": (torch.float32, n), "g": (torch.float32, n), "m": (moment, n), "v": (moment, n)}
+        if cfg.moment_bits == 8:
+            wanted.update(m_power=(torch.uint8, powers), v_power=(torch.uint8, powers))
+        half = t.get("half")
+        if half is not None:
+            if half.dtype not in (torch.bfloat16, torch.float16):
+                raise MoeError(f"moe_adamw_plan: half is {half.dtype}")
+            wanted["half"] = (half.dtype, n)
+        for name, (dtype, size) in wanted.items():
+            a = t[name]
+            if a.dtype != dtype or a.numel() != size or not a.is_contiguous() or not a.is_cuda:
+                raise MoeError(f"moe_adamw_plan: {name} must be a contiguous device tensor of {size} elements of {dtype}")
+            if device is None:
+                device = a.device
+            if a.device != device:
+                raise MoeError("moe_adamw_plan: tensors on different devices")
+            setattr(entry, name, a.data_ptr())
+        entry.n = n
+        entry.half_dtype = MOE_F16 if half is not None and half.dtype == torch.float16 else MOE_BF16
+        entry.lr_scale = float(t.get("lr_scale", 1.0))
+        entry.weight_decay = float(t.get("weight_decay", 0.0))
+    lib = load_library()
+    size = lib.moe_adamw_plan_bytes(byref(cfg), table, len(tensors))
+    host, chunks = torch.zeros(max(size, 16), dtype=torch.uint8), c_int64(0)
+    _check(lib.moe_adamw_plan(byref(cfg), table, len(tensors), _ptr(host), _nbytes(host), byref(chunks)), "moe_adamw_plan")
+    return AdamwPlan(host.to(device or "cuda"), len(tensors), chunks.value, list(tensors))
+
+
+def moe_adamw_scalars(step, lr, grad_scale=1.0, skip=False, out=None):
+    """The values of a step in device memory (int32 step and skip, float32 lr and grad_scale); `out`: such a tensor, overwritten."""
+    import torch
+    host = torch.empty(4, dtype=torch.int32)
+    host[0], host[1] = int(step), int(bool(skip))
+    host[2:].view(torch.float32).copy_(torch.tensor([lr, grad_scale], dtype=torch.float32))
+    return host.cuda() if out is None else out.copy_(host)
+
+
+def moe_adamw_step(cfg, plan, values, stream=None):
+    _check(load_library().moe_adamw_step(byref(cfg), _ptr(plan.memory), plan.n_tensors, plan.n_chunks, _ptr(values),
+                                         _stream(stream)), "moe_adamw_step")
 
 
 def moe_copy_bytes(src, dst, stream=None):

@@ -103,6 +103,7 @@ const char* moe_status_string(int status) {
     case MOE_ERR_ALIGN: return "a device pointer is not 16-byte aligned";
     case MOE_ERR_WORKSPACE: return "workspace too small";
     case MOE_ERR_HIP: return "a HIP runtime call failed";
+    case MOE_ERR_OVERLAP: return "memory that the call would write is named twice";
     default: return "unknown status";
   }
 }
