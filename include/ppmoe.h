@@ -337,6 +337,48 @@ int moe_layer_forward_aux(const moe_config* cfg, const void* x, const void* Wg, 
                           int32_t* first_counts, void* workspace, size_t workspace_bytes,
                           void* const* stage_events, void* stream);
 
+/* Low-rank adapters of many requests beside the experts' projections (Section 3.3.2: the local experts' matrices, here
+ * frozen).  Row r of the packed rows offsets[i] <= r < offsets[i+1] belongs to expert i, as moe_slice_dispatch
+ * leaves them (n_exp == 1: a dense projection, offsets = {0, rows}); its token is perm[r] / top_k, or r when perm is NULL; the
+ * token's adapter is a = adapter[token], and an index outside [0, n_adapters) means none.
+ *   v[r, :] = A[a][i] x[r, :]                                          [rank]  float32, 0 without an adapter
+ *   u[r, :] = W[i] x[r, :] + scale[a] B[a][i] v[r, :]                   [N]
+ *   y[r, :] = u[r, :], or GeLU(u[r, :]) (tanh form) with MOE_ACT_GELU
+ * W [n_exp, N, K], A [n_adapters, n_exp, rank, K], B [n_adapters, n_exp, N, rank], x [rows, K], y [rows, N] in dtype (BF16 or
+ * F16); scale [n_adapters] float32, or NULL for ones; adapter [tokens], perm [rows], offsets [n_exp + 1] int32; v [rows, rank] float32.
+ * All products are accumulated in float32 and y is rounded once.  scale v enters the second product in dtype (so it has to
+ * be within an fp16 number's range with F16).  Infinities and NaNs in an adapter's A or B reach rows of that adapter alone (B's as
+ * NaN, and up to 31 columns beside them with them); rows without an adapter have the bits they would have without any.
+ * rows is the most there are: rows at or beyond offsets[n_exp] are neither read nor written.
+ * Limits: rows >= 0, K and N multiples of 8 up to 2^20, n_exp <= 256, n_exp * n_adapters <= 65536, rank a multiple of 8 up to 128,
+ * top_k <= 8.
+ * moe_adapter_backward, from dy = dLoss/du (activation MOE_ACT_NONE only) and the v the forward left:
+ *   t[r, :]  = scale[a] B[a][i]^T dy[r, :]
+ *   dx[r, :] = W[i]^T dy[r, :] + A[a][i]^T t[r, :]              [rows, K] dtype; not computed when dx is NULL
+ *   dA[a][i] = sum over its rows of t[r, :] x[r, :]^T              [n_adapters, n_exp, rank, K] float32
+ *   dB[a][i] = sum over its rows of dy[r, :] (scale[a] v[r, :])^T   [n_adapters, n_exp, N, rank] float32
+ * dA and dB are overwritten in full (zeros for a pair without rows) and hold float32 accuracy: t and v enter as two 16-bit summands.
+ * Sums have a fixed order: the same bits on every run.  Neither call allocates or, after moe_init, synchronises.
+ * workspace: at least moe_adapter_workspace_bytes / moe_adapter_backward_workspace_bytes bytes (0 on an invalid config); calls
+ * that share one must be ordered on one stream. */
+enum { MOE_ACT_NONE = 0, MOE_ACT_GELU = 1 };
+typedef struct {
+  int32_t rows, K, N;
+  int32_t n_exp, n_adapters, rank;
+  int32_t top_k;            /* of the dispatch that made perm; 1 without one */
+  int32_t dtype;            /* MOE_BF16 or MOE_F16 */
+  int32_t activation;       /* MOE_ACT_NONE or MOE_ACT_GELU */
+} moe_adapter_config;
+size_t moe_adapter_workspace_bytes(const moe_adapter_config* cfg);
+int moe_adapter_forward(const moe_adapter_config* cfg, const void* x, const int32_t* offsets, const void* W, const void* A,
+                        const void* B, const float* scale, const int32_t* adapter, const int32_t* perm, void* y, float* v,
+                        void* workspace, size_t workspace_bytes, void* stream);
+size_t moe_adapter_backward_workspace_bytes(const moe_adapter_config* cfg);
+int moe_adapter_backward(const moe_adapter_config* cfg, const void* x, const int32_t* offsets, const void* W, const void* A,
+                         const void* B, const float* scale, const int32_t* adapter, const int32_t* perm, const void* dy,
+                         const float* v, void* dx, float* dA, float* dB, void* workspace, size_t workspace_bytes,
+                         void* stream);
+
 /* Optimizer step (Section 4.1: Adam with float32 master weights and moments): AdamW over many tensors, one launch.
  * With g = grad * grad_scale, t the step and per tensor lr = values.lr * lr_scale:
  *   m' = beta1 m + (1 - beta1) g                 v' = beta2 v + (1 - beta2) g^2

@@ -28,6 +28,10 @@ class MoeWorkspaceLayout(Structure):
                                         "logits", "aux")]
 
 
+class MoeAdapterConfig(Structure):
+    _fields_ = [(n, c_int32) for n in ("rows", "K", "N", "n_exp", "n_adapters", "rank", "top_k", "dtype", "activation")]
+
+
 class MoeAdamwConfig(Structure):
     _fields_ = [("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("moment_bits", c_int32),
                 ("reserved", c_int32)]
@@ -76,6 +80,10 @@ _PROTOTYPES = {
     "moe_layer_forward": (c_int, [POINTER(MoeConfig)] + [c_void_p] * 7 + [c_size_t, POINTER(c_void_p), c_void_p]),
     "moe_layer_forward_aux": (c_int, [POINTER(MoeConfig)] + [c_void_p] * 10 + [c_size_t, POINTER(c_void_p), c_void_p]),
     "moe_layer_fuses": (c_int, [POINTER(MoeConfig)]),
+    "moe_adapter_workspace_bytes": (c_size_t, [POINTER(MoeAdapterConfig)]),
+    "moe_adapter_forward": (c_int, [POINTER(MoeAdapterConfig)] + [c_void_p] * 11 + [c_size_t, c_void_p]),
+    "moe_adapter_backward_workspace_bytes": (c_size_t, [POINTER(MoeAdapterConfig)]),
+    "moe_adapter_backward": (c_int, [POINTER(MoeAdapterConfig)] + [c_void_p] * 14 + [c_size_t, c_void_p]),
     "moe_adamw_plan_bytes": (c_size_t, [POINTER(MoeAdamwConfig), POINTER(MoeAdamwTensor), c_int32]),
     "moe_adamw_plan": (c_int, [POINTER(MoeAdamwConfig), POINTER(MoeAdamwTensor), c_int32, c_void_p, c_size_t,
                                POINTER(c_int64)]),
@@ -340,6 +348,36 @@ MOE_FUSE_SLICE, MOE_FUSE_COMBINE = 1, 2
 def moe_layer_fuses(cfg) -> int:
     """Mask of MOE_FUSE_SLICE / MOE_FUSE_COMBINE: the stages moe_layer_forward folds into the GEMMs."""
     return load_library().moe_layer_fuses(byref(cfg))
+
+
+MOE_ACT_NONE, MOE_ACT_GELU = 0, 1
+
+
+def make_adapter_config(rows, K, N, n_exp, n_adapters, rank, top_k=1, dtype="bf16", gelu=False) -> MoeAdapterConfig:
+    code = {"f32": MOE_F32, "bf16": MOE_BF16, "f16": MOE_F16}
+    return MoeAdapterConfig(rows, K, N, n_exp, n_adapters, rank, top_k, code[dtype], MOE_ACT_GELU if gelu else MOE_ACT_NONE)
+
+
+def moe_adapter_workspace_bytes(cfg) -> int:
+    return load_library().moe_adapter_workspace_bytes(byref(cfg))
+
+
+def moe_adapter_forward(cfg, x, offsets, W, A, B, scale, adapter, perm, y, v, workspace, stream=None):
+    """The grouped projection with each row's adapter beside it (scale and perm may be None)."""
+    _check(load_library().moe_adapter_forward(
+        byref(cfg), _ptr(x), _ptr(offsets), _ptr(W), _ptr(A), _ptr(B), _ptr(scale), _ptr(adapter), _ptr(perm), _ptr(y), _ptr(v),
+        _ptr(workspace), _nbytes(workspace), _stream(stream)), "moe_adapter_forward")
+
+
+def moe_adapter_backward_workspace_bytes(cfg) -> int:
+    return load_library().moe_adapter_backward_workspace_bytes(byref(cfg))
+
+
+def moe_adapter_backward(cfg, x, offsets, W, A, B, scale, adapter, perm, dy, v, dx, dA, dB, workspace, stream=None):
+    """Its gradients with W frozen (scale, perm and dx may be None); dA and dB are float32 and overwritten."""
+    _check(load_library().moe_adapter_backward(
+        byref(cfg), _ptr(x), _ptr(offsets), _ptr(W), _ptr(A), _ptr(B), _ptr(scale), _ptr(adapter), _ptr(perm), _ptr(dy), _ptr(v),
+        _ptr(dx), _ptr(dA), _ptr(dB), _ptr(workspace), _nbytes(workspace), _stream(stream)), "moe_adapter_backward")
 
 
 def make_adamw_config(beta1=0.9, beta2=0.999, eps=1e-8, moment_bits=32) -> MoeAdamwConfig:

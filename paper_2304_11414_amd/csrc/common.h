@@ -148,6 +148,14 @@ struct Elem16<MOE_F16> {
 };
 inline bool is_16bit(int dtype) { return dtype == MOE_BF16 || dtype == MOE_F16; }
 
+// What a grouped product adds to its rows for their adapters (adapter_core.h); of_row[r]: the adapter of packed row r, or -1.
+struct AdapterRows {
+  const int32_t* of_row;
+  const bf16_t* low;
+  const bf16_t* up;
+  int n_exp, rank;
+};
+
 // Launchers (host).  Each returns the hipError_t of its last launch.
 hipError_t launch_gate(const moe_config& c, const void* x, const void* Wg, const float* bias,
                        const float* logits_in, float* logits_out, int32_t* expert_idx,
@@ -216,7 +224,14 @@ hipError_t launch_grouped_gemm(int in_dtype, bool gelu, const void* A, const voi
                                const int32_t* offsets, int n_exp, int64_t max_rows, int Nout, int K,
                                void* workspace, hipStream_t s, int fuse = 0,
                                const int32_t* aux_rows = nullptr, const float* aux_w = nullptr,
-                               int aux_div = 1, const int32_t* aux_inv = nullptr, void* C2 = nullptr);
+                               int aux_div = 1, const int32_t* aux_inv = nullptr, void* C2 = nullptr,
+                               const AdapterRows* adapters = nullptr);
+// (adapters: added before the activation; 16-bit types, no fuse)
+// cc[r, 0..n) = a[r, 0..k) b[i] with b [n_exp, k, n], 16-bit types (the data gradients).  rows: the host's bound;
+// expected_rows: fewer where a rank holds some of the experts that the rows may go to.
+hipError_t launch_data_gradient(int dtype, const bf16_t* a, const bf16_t* b, bf16_t* cc, const int32_t* offsets, int n_exp,
+                                int64_t rows, int64_t expected_rows, int n, int k, void* gemm_ws, hipStream_t s,
+                                const AdapterRows* adapters = nullptr);
 // Backward of the expert FFN on the packed rows (16-bit types only): dX [rows, d] 16-bit,
 // dW1 [n_exp, F, d] and dW2 [n_exp, d, F] float32; scratch: expert_ffn_backward_scratch_bytes bytes.
 size_t expert_ffn_backward_scratch_bytes(const moe_config& c, int64_t rows);
@@ -267,7 +282,7 @@ hipError_t launch_grouped_gemm_few_rows(int in_dtype, bool gelu, const bf16_t* A
                                         const int32_t* offsets, int n_exp, int Nout, int K, int most,
                                         void* workspace, hipStream_t s, int fuse, const int32_t* aux_rows,
                                         const float* aux_w, int aux_div,
-                                        const int32_t* aux_inv, bf16_t* C2);
+                                        const int32_t* aux_inv, bf16_t* C2, const AdapterRows* adapters = nullptr);
 // Where in a GEMM workspace a block leaves its clocks (four words: shader and wall clock, start and end).
 unsigned long long* gemm_clock_words(void* workspace);
 // The most rows one expert may have for that kernel to be taken; 0: it is not taken whatever the counts.  With at most
@@ -344,7 +359,8 @@ hipError_t launch_grouped_gemm_fast(int in_dtype, bool gelu, const bf16_t* A, co
                                     const int32_t* offsets, int n_exp, int few_most, int Nout,
                                     int K, void* workspace, hipStream_t s, int fuse,
                                     const int32_t* aux_rows, const float* aux_w, int aux_div,
-                                    const int32_t* aux_inv, bf16_t* C2, bool b_by_rows = false, int pick_cus = 0);
+                                    const int32_t* aux_inv, bf16_t* C2, bool b_by_rows = false, int pick_cus = 0,
+                                    const AdapterRows* adapters = nullptr);
 
 // Most segments the permutation can be asked for: kSegment assignments each when it counts them
 // itself, the tokens of one wavefront of the gating kernel each when that kernel counts them.

@@ -16,7 +16,7 @@
 // The tile list is built on the device from offsets[]: a block decodes its (expert, m-tile, n-tile)
 // from blockIdx, blocks beyond the real tile count exit at once.  No host round trip.
 
-#include "common.h"
+#include "adapter_core.h"
 
 namespace ppmoe {
 
@@ -94,10 +94,10 @@ constexpr int kTileBytes = kBM * kBK * 2;  // one operand tile in LDS: 32 KiB
 // XOR-swizzled with the row number.
 __device__ __forceinline__ int lds_piece(int row, int ch) { return row * 128 + ((ch ^ ((row >> 1) & 7)) << 4); }
 
-template <bool GELU, int DT>
+template <bool GELU, int DT, bool ADAPT>
 __global__ __launch_bounds__(kGemmThreads) void grouped_gemm_bf16_kernel(
     const bf16_t* __restrict__ A, const bf16_t* __restrict__ B, bf16_t* __restrict__ C,
-    const int32_t* __restrict__ offsets, int n_exp, int Nout, int K) {
+    const int32_t* __restrict__ offsets, int n_exp, int Nout, int K, AdapterRows adapters) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];  // 2 stages x (A tile + B tile)
 
   const int n_tiles = (Nout + kBN - 1) / kBN;
@@ -188,6 +188,9 @@ __global__ __launch_bounds__(kGemmThreads) void grouped_gemm_bf16_kernel(
     if (kt + 1 < KT) store_lds(stage ^ 1);
     __syncthreads();
   }
+
+  if constexpr (ADAPT)
+    add_low_rank<DT, 32, 4, 2>(acc, adapters, tc.expert, tc.row0 + wm * 128, tc.rows - wm * 128, tc.col0 + wn * 64, Nout);
 
   // ---- epilogue ------------------------------------------------------------------------------
   // D = W_frag (32 n) x Tok_frag^T (32 m): lane holds token column m = lane % 32 and, in register
@@ -339,10 +342,12 @@ constexpr int64_t kF32WideTiles = 512;
 static hipError_t ensure_lds_attr() {
   static std::atomic<uint64_t> done{0};
   return once_per_device(done, [] {
-    const void* kernels[] = {reinterpret_cast<const void*>(grouped_gemm_bf16_kernel<true, MOE_BF16>),
-                             reinterpret_cast<const void*>(grouped_gemm_bf16_kernel<false, MOE_BF16>),
-                             reinterpret_cast<const void*>(grouped_gemm_bf16_kernel<true, MOE_F16>),
-                             reinterpret_cast<const void*>(grouped_gemm_bf16_kernel<false, MOE_F16>)};
+#define PPMOE_KERNELS(DT, ADAPT)                                                 \
+  reinterpret_cast<const void*>(grouped_gemm_bf16_kernel<true, DT, ADAPT>),      \
+      reinterpret_cast<const void*>(grouped_gemm_bf16_kernel<false, DT, ADAPT>)
+    const void* kernels[] = {PPMOE_KERNELS(MOE_BF16, false), PPMOE_KERNELS(MOE_BF16, true), PPMOE_KERNELS(MOE_F16, false),
+                             PPMOE_KERNELS(MOE_F16, true)};
+#undef PPMOE_KERNELS
     for (const void* k : kernels) {
       hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, 4 * kTileBytes);
       if (e != hipSuccess) return e;
@@ -354,20 +359,22 @@ static hipError_t ensure_lds_attr() {
 hipError_t launch_grouped_gemm(int in_dtype, bool gelu, const void* A, const void* B, void* C,
                                const int32_t* offsets, int n_exp, int64_t max_rows, int Nout, int K,
                                void* workspace, hipStream_t s, int fuse, const int32_t* aux_rows,
-                               const float* aux_w, int aux_div, const int32_t* aux_inv, void* C2) {
+                               const float* aux_w, int aux_div, const int32_t* aux_inv, void* C2, const AdapterRows* adapters) {
   if (max_rows == 0) return hipSuccess;
+  if (adapters != nullptr && (!is_16bit(in_dtype) || fuse != 0)) return hipErrorInvalidValue;
   const int few_most = grouped_gemm_few_rows_most(in_dtype, Nout, K, max_rows, n_exp);
   if (few_most > 0) {
     const bool sure = max_rows <= few_most;   // else both are launched, and one of them leaves (5 us and a gap)
     const hipError_t e = launch_grouped_gemm_few_rows(
         in_dtype, gelu, static_cast<const bf16_t*>(A), static_cast<const bf16_t*>(B), static_cast<bf16_t*>(C), offsets,
-        n_exp, Nout, K, sure ? 0 : few_most, workspace, s, fuse, aux_rows, aux_w, aux_div, aux_inv, static_cast<bf16_t*>(C2));
+        n_exp, Nout, K, sure ? 0 : few_most, workspace, s, fuse, aux_rows, aux_w, aux_div, aux_inv, static_cast<bf16_t*>(C2),
+        adapters);
     if (e != hipSuccess || sure) return e;
   }
   if (grouped_gemm_is_fast(in_dtype, K)) {
     return launch_grouped_gemm_fast(in_dtype, gelu, static_cast<const bf16_t*>(A), static_cast<const bf16_t*>(B),
                                     static_cast<bf16_t*>(C), offsets, n_exp, few_most, Nout, K, workspace, s,
-                                    fuse, aux_rows, aux_w, aux_div, aux_inv, static_cast<bf16_t*>(C2));
+                                    fuse, aux_rows, aux_w, aux_div, aux_inv, static_cast<bf16_t*>(C2), false, 0, adapters);
   }
   if (fuse != 0) return hipErrorInvalidValue;   // the other kernels work on packed tensors only
   if (is_16bit(in_dtype)) {
@@ -380,9 +387,15 @@ hipError_t launch_grouped_gemm(int in_dtype, bool gelu, const void* A, const voi
     const bf16_t* a = static_cast<const bf16_t*>(A);
     const bf16_t* b = static_cast<const bf16_t*>(B);
     bf16_t* c = static_cast<bf16_t*>(C);
-#define PPMOE_GEMM16(G, DT)                                                                         \
-  grouped_gemm_bf16_kernel<G, DT><<<static_cast<unsigned>(grid), kGemmThreads, 4 * kTileBytes, s>>>( \
-      a, b, c, offsets, n_exp, Nout, K)
+    const AdapterRows rows = adapters != nullptr ? *adapters : AdapterRows{};
+#define PPMOE_GEMM16_A(G, DT, ADAPT)                                                                        \
+  grouped_gemm_bf16_kernel<G, DT, ADAPT><<<static_cast<unsigned>(grid), kGemmThreads, 4 * kTileBytes, s>>>( \
+      a, b, c, offsets, n_exp, Nout, K, rows)
+#define PPMOE_GEMM16(G, DT)                              \
+  do {                                                   \
+    if (adapters != nullptr) PPMOE_GEMM16_A(G, DT, true); \
+    else PPMOE_GEMM16_A(G, DT, false);                   \
+  } while (0)
     if (in_dtype == MOE_F16) {
       if (gelu) PPMOE_GEMM16(true, MOE_F16);
       else PPMOE_GEMM16(false, MOE_F16);
@@ -391,6 +404,7 @@ hipError_t launch_grouped_gemm(int in_dtype, bool gelu, const void* A, const voi
       else PPMOE_GEMM16(false, MOE_BF16);
     }
 #undef PPMOE_GEMM16
+#undef PPMOE_GEMM16_A
   } else {
     auto tiles = [&](int t) -> int64_t { return ((max_rows + t - 1) / t + n_exp) * ((Nout + t - 1) / t); };
     const bool wide = ((max_rows + 63) / 64) * ((Nout + 63) / 64) >= kF32WideTiles;

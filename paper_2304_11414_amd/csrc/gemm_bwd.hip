@@ -24,6 +24,7 @@
 
 #include <type_traits>
 
+#include "adapter_core.h"
 #include "gemm_core.h"
 
 namespace ppmoe {
@@ -287,10 +288,11 @@ __device__ __forceinline__ void accumulate_tile(const TileInfo& ti, f32x16 (&acc
 //                           A [rows, K] 16-bit, B [n_exp, K, N] 16-bit, C [rows, N] 16-bit
 // MODE 1 (weight gradient): C[i][m, n] = sum_{r in expert i} A[r, m] * B[r, n]
 //                           A [rows, M] 16-bit, B [rows, N] 16-bit, C [n_exp, M, N] float32
-template <int MODE, int DT>
+// ADAPT (MODE 0): the rows' adapters are added (adapter_core.h).
+template <int MODE, int DT, bool ADAPT = false>
 __global__ __launch_bounds__(kThreads) void grouped_gemm_bwd_kernel(
     const bf16_t* __restrict__ A, const bf16_t* __restrict__ B, void* __restrict__ C,
-    const int32_t* __restrict__ offsets, int n_exp, int M, int N, int K, int pick_cus) {
+    const int32_t* __restrict__ offsets, int n_exp, int M, int N, int K, int pick_cus, AdapterRows adapters) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   TileInfo ti;
   if (MODE == 0 && pick_cus > 0 && !few_big_tiles(offsets, n_exp, N, K, pick_cus)) return;
@@ -298,6 +300,9 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_bwd_kernel(
   f32x16 acc[2][2];
   accumulate_tile<MODE, DT>(ti, acc, lds);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if constexpr (ADAPT)
+    add_low_rank<DT, 32, 2, 2>(acc, adapters, ti.expert, ti.row0 + (wave >> 1) * 64, ti.rows - (wave >> 1) * 64,
+                               ti.col0 + (wave & 1) * 64, N);
   store_tile_output<MODE, DT>(acc, C, ti, N, M, wave >> 1, wave & 1, lane & 31, lane >> 5);
 }
 
@@ -567,6 +572,69 @@ static int cus_of_current_device() {
   return cus;
 }
 
+static hipError_t ensure_backward_attrs() {
+  using namespace bwd;
+  static std::atomic<uint64_t> attrs_done{0};
+  return once_per_device(attrs_done, [] {
+    const void* small[] = {reinterpret_cast<const void*>(grouped_gemm_bwd_kernel<0, MOE_BF16>),
+                           reinterpret_cast<const void*>(grouped_gemm_bwd_kernel<0, MOE_BF16, true>),
+                           reinterpret_cast<const void*>(grouped_gemm_bwd_kernel<0, MOE_F16, true>),
+                           reinterpret_cast<const void*>(grouped_gemm_bwd_kernel<1, MOE_BF16>),
+                           reinterpret_cast<const void*>(grouped_gemm_bwd_kernel<0, MOE_F16>),
+                           reinterpret_cast<const void*>(grouped_gemm_bwd_kernel<1, MOE_F16>)};
+    const void* big[] = {reinterpret_cast<const void*>(weight_gradient_kernel<MOE_BF16>),
+                         reinterpret_cast<const void*>(weight_gradient_kernel<MOE_F16>)};
+    for (const void* k : small) {
+      hipError_t err = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kPlainLdsBytes);
+      if (err != hipSuccess) return err;
+    }
+    for (const void* k : big) {
+      hipError_t err = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kWgradLdsBytes);
+      if (err != hipSuccess) return err;
+    }
+    return hipSuccess;
+  });
+}
+
+// An operand by rows on the persistent kernels: 32-bit offsets up to 63 rows past a k-tile's first (63 * 2^25 + 512 < 2^31,
+// where the descriptors end); beyond that the 128 x 128 tiles, whose offsets have 64 bits.
+constexpr int kColumnsByRows = 1 << 24;
+
+// The persistent kernel takes contractions of whole k-tiles, unless that
+// would leave more than half of the CUs without a tile; then 128 x 128 tiles, two blocks per CU.  The host knows the row
+// count only as a bound (the counts live on the device).  Where the rank holds some of the experts that is every
+// assignment there is: if an even share of them would be too few tiles, both shapes are launched and the row counts decide
+// (few_big_tiles; the launch that leaves costs about 5 us).
+hipError_t launch_data_gradient(int dtype, const bf16_t* a, const bf16_t* b, bf16_t* cc, const int32_t* offsets, int n_exp,
+                                int64_t rows, int64_t expected_rows, int n, int k, void* gemm_ws, hipStream_t s,
+                                const AdapterRows* adapters) {
+  using namespace bwd;
+  if (rows == 0) return hipSuccess;
+  hipError_t e = ensure_backward_attrs();
+  if (e != hipSuccess) return e;
+  const int n_cus = cus_of_current_device() & ~7;
+  auto few = [&](int64_t r) { return 2 * ((r + 255) / 256 + n_exp) * ((n + 255) / 256) < n_cus; };
+  const bool big = k % BK == 0 && k < (1 << 22) && n < kColumnsByRows && !few(rows);
+  const int pick_cus = big && expected_rows < rows && few(expected_rows) ? n_cus : 0;
+  if (big) {
+    e = launch_grouped_gemm_fast(dtype, false, a, b, cc, offsets, n_exp, 0, n, k, gemm_ws, s, 0, nullptr, nullptr, 1, nullptr,
+                                 nullptr, true, pick_cus, adapters);
+    if (e != hipSuccess || pick_cus == 0) return e;
+  }
+  // (as a second shape it has fewer than n_cus / 2 tiles of 256 x 256 to do, each four of its own)
+  const int64_t tiles = big ? 2 * n_cus : ((rows + 127) / 128 + n_exp) * ((n + 127) / 128);
+  const unsigned grid = static_cast<unsigned>((tiles + 7) / 8 * 8);
+  const AdapterRows ad = adapters != nullptr ? *adapters : AdapterRows{};
+#define PPMOE_LAUNCH(DT, ADAPT) \
+  grouped_gemm_bwd_kernel<0, DT, ADAPT><<<grid, kThreads, kPlainLdsBytes, s>>>(a, b, cc, offsets, n_exp, 0, n, k, pick_cus, ad)
+  if (dtype == MOE_F16 && adapters != nullptr) PPMOE_LAUNCH(MOE_F16, true);
+  else if (dtype == MOE_F16) PPMOE_LAUNCH(MOE_F16, false);
+  else if (adapters != nullptr) PPMOE_LAUNCH(MOE_BF16, true);
+  else PPMOE_LAUNCH(MOE_BF16, false);
+#undef PPMOE_LAUNCH
+  return hipGetLastError();
+}
+
 size_t expert_ffn_backward_gemm_offset(const moe_config& c, int64_t rows) {
   // U, H, dU: three [rows, F] 16-bit buffers (256-byte aligned), then the persistent GEMM's scratch
   return 3 * ((static_cast<size_t>(rows) * c.F * 2 + 255) & ~size_t(255));
@@ -604,51 +672,11 @@ hipError_t launch_expert_ffn_backward(const moe_config& c, int64_t rows, const v
   }
 
   const int n_cus = cus_of_current_device() & ~7;
-  static std::atomic<uint64_t> attrs_done{0};
-  const hipError_t attrs = once_per_device(attrs_done, [] {
-    const void* small[] = {reinterpret_cast<const void*>(grouped_gemm_bwd_kernel<0, MOE_BF16>),
-                           reinterpret_cast<const void*>(grouped_gemm_bwd_kernel<1, MOE_BF16>),
-                           reinterpret_cast<const void*>(grouped_gemm_bwd_kernel<0, MOE_F16>),
-                           reinterpret_cast<const void*>(grouped_gemm_bwd_kernel<1, MOE_F16>)};
-    const void* big[] = {reinterpret_cast<const void*>(weight_gradient_kernel<MOE_BF16>),
-                         reinterpret_cast<const void*>(weight_gradient_kernel<MOE_F16>)};
-    for (const void* k : small) {
-      hipError_t err = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kPlainLdsBytes);
-      if (err != hipSuccess) return err;
-    }
-    for (const void* k : big) {
-      hipError_t err = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kWgradLdsBytes);
-      if (err != hipSuccess) return err;
-    }
-    return hipSuccess;
-  });
+  const hipError_t attrs = ensure_backward_attrs();
   if (attrs != hipSuccess) return attrs;
-  // An operand by rows on the persistent kernels: 32-bit offsets up to 63 rows past a k-tile's first (63 * 2^25 + 512 < 2^31,
-  // where the descriptors end); beyond that the 128 x 128 tiles, whose offsets have 64 bits.
-  constexpr int kColumnsByRows = 1 << 24;
-  // cc[rows, n] = a[rows, k] b[i][k, n].  The persistent kernel takes contractions of whole k-tiles, unless that
-  // would leave more than half of the CUs without a tile; then 128 x 128 tiles, two blocks per CU.  The host knows the row
-  // count only as a bound (the counts live on the device).  Where the rank holds some of the experts that is every
-  // assignment there is: if an even share of them would be too few tiles, both shapes are launched and the row counts decide
-  // (few_big_tiles; the launch that leaves costs about 5 us).
+  // cc[rows, n] = a[rows, k] b[i][k, n]
   auto data_gradient = [&](const bf16_t* a, const bf16_t* b, bf16_t* cc, int n, int k) -> hipError_t {
-    if (rows == 0) return hipSuccess;
-    auto few = [&](int64_t r) { return 2 * ((r + 255) / 256 + N) * ((n + 255) / 256) < n_cus; };
-    const bool big = k % BK == 0 && k < (1 << 22) && n < kColumnsByRows && !few(rows);
-    const int pick_cus = big && N < c.E && few(rows * N / c.E) ? n_cus : 0;
-    if (big) {
-      const hipError_t e = launch_grouped_gemm_fast(c.in_dtype, false, a, b, cc, offsets, N, 0, n, k, gemm_ws, s, 0, nullptr,
-                                                    nullptr, 1, nullptr, nullptr, true, pick_cus);
-      if (e != hipSuccess || pick_cus == 0) return e;
-    }
-    // (as a second shape it has fewer than n_cus / 2 tiles of 256 x 256 to do, each four of its own)
-    const int64_t tiles = big ? 2 * n_cus : ((rows + 127) / 128 + N) * ((n + 127) / 128);
-    const unsigned grid = static_cast<unsigned>((tiles + 7) / 8 * 8);
-    if (c.in_dtype == MOE_F16)
-      grouped_gemm_bwd_kernel<0, MOE_F16><<<grid, kThreads, kPlainLdsBytes, s>>>(a, b, cc, offsets, N, 0, n, k, pick_cus);
-    else
-      grouped_gemm_bwd_kernel<0, MOE_BF16><<<grid, kThreads, kPlainLdsBytes, s>>>(a, b, cc, offsets, N, 0, n, k, pick_cus);
-    return hipGetLastError();
+    return launch_data_gradient(c.in_dtype, a, b, cc, offsets, N, rows, N < c.E ? rows * N / c.E : rows, n, k, gemm_ws, s);
   };
   // cc[i][m, n] = sum over the rows of expert i of a[r, m] b[r, n].  The persistent kernel (one block per CU) unless
   // that would leave more than half of the CUs without a tile; then 128 x 128 tiles, two blocks per CU.
@@ -663,9 +691,9 @@ hipError_t launch_expert_ffn_backward(const moe_config& c, int64_t rows, const v
     const int64_t small_tiles = static_cast<int64_t>(N) * ((m + 127) / 128) * ((n + 127) / 128);
     const unsigned grid = static_cast<unsigned>((small_tiles + 7) / 8 * 8);
     if (c.in_dtype == MOE_F16)
-      grouped_gemm_bwd_kernel<1, MOE_F16><<<grid, kThreads, kPlainLdsBytes, s>>>(a, b, cc, offsets, N, m, n, 0, 0);
+      grouped_gemm_bwd_kernel<1, MOE_F16><<<grid, kThreads, kPlainLdsBytes, s>>>(a, b, cc, offsets, N, m, n, 0, 0, AdapterRows{});
     else
-      grouped_gemm_bwd_kernel<1, MOE_BF16><<<grid, kThreads, kPlainLdsBytes, s>>>(a, b, cc, offsets, N, m, n, 0, 0);
+      grouped_gemm_bwd_kernel<1, MOE_BF16><<<grid, kThreads, kPlainLdsBytes, s>>>(a, b, cc, offsets, N, m, n, 0, 0, AdapterRows{});
     return hipGetLastError();
   };
 

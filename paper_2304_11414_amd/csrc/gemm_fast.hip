@@ -33,6 +33,7 @@
 #include <atomic>
 #include <mutex>
 
+#include "adapter_core.h"
 #include "gemm_core.h"
 
 namespace ppmoe {
@@ -126,13 +127,14 @@ __global__ __launch_bounds__(kThreads) void xcc_probe_kernel() {
 // B_BY_ROWS: B is [n_exp, K, Nout] (its contraction index is its row): the data gradients of the backward pass.
 // ACT: 0: no activation; 1: GeLU; 2: the pre-activations are stored as C2, and GeLU of them as stored (see gelu_sigmoid) as C
 // (no FUSE): a training step keeps both.
-template <int ACT, int FUSE, int DT, bool RAGGED, bool B_BY_ROWS>
+// ADAPT: the rows' adapters are added to a tile's accumulators (adapter_core.h) by the CU that holds its first k-tile.
+template <int ACT, int FUSE, int DT, bool RAGGED, bool B_BY_ROWS, bool ADAPT = false>
 __global__ __launch_bounds__(kThreads) void grouped_gemm_fast_kernel(
     const bf16_t* __restrict__ A, const bf16_t* __restrict__ B, bf16_t* __restrict__ C,
     const int32_t* __restrict__ offsets, int n_exp, int few_most, int Nout, int K, float* __restrict__ slots,
     uint32_t* __restrict__ flags, uint32_t epoch, int same_l2, int spin_limit,
     const int32_t* __restrict__ aux_rows, const float* __restrict__ aux_w, int aux_div,
-    const int32_t* __restrict__ aux_inv, bf16_t* __restrict__ C2, int pick_cus) {
+    const int32_t* __restrict__ aux_inv, bf16_t* __restrict__ C2, int pick_cus, AdapterRows adapters) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   __shared__ int contrib[kMaxPersistentBlocks / 8 + 1];   // [0] = how many, then the block ids whose slots to add
   __shared__ int contrib_failed;
@@ -909,6 +911,9 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_fast_kernel(
 #pragma unroll
         for (int ni = 0; ni < 8; ++ni) acc[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
       k_loop<DT, false, B_BY_ROWS, kStores>(acc, a_base, b_base, tiles, stores_behind, load_big);
+      if constexpr (ADAPT)
+        if (cur.kb == 0)
+          add_low_rank<DT, 16, 8, 8>(acc, adapters, cur.expert, cur.row0 + wm * 128, cur.rows - wm * 128, cur.col0 + wn * 128, Nout);
       finish_segment(acc, IC<8>{});
     } else {
       f32x4 acc[8][4];
@@ -919,6 +924,8 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_fast_kernel(
       if (cur.kind == 1) small_loop(IC<1>{}, acc, tiles, stores_behind);
       else if (cur.kind == 2) small_loop(IC<2>{}, acc, tiles, stores_behind);
       else small_loop(IC<4>{}, acc, tiles, stores_behind);
+      if constexpr (ADAPT)
+        if (cur.kb == 0) add_low_rank<DT, 16, 8, 4>(acc, adapters, cur.expert, cur.row0, cur.rows, cur.col0 + wave * 64, Nout);
       finish_segment(acc, IC<4>{});
     }
   }
@@ -1009,12 +1016,20 @@ hipError_t setup_attrs(FastSetup& st, int dev) {
       reinterpret_cast<const void*>(grouped_gemm_fast_kernel<0, 0, DT, R, false>),     \
       reinterpret_cast<const void*>(grouped_gemm_fast_kernel<1, 1, DT, R, false>),      \
       reinterpret_cast<const void*>(grouped_gemm_fast_kernel<0, 2, DT, R, false>)
+#define PPMOE_ADAPTED(DT)                                                                  \
+  reinterpret_cast<const void*>(grouped_gemm_fast_kernel<1, 0, DT, false, false, true>),   \
+      reinterpret_cast<const void*>(grouped_gemm_fast_kernel<0, 0, DT, false, false, true>), \
+      reinterpret_cast<const void*>(grouped_gemm_fast_kernel<1, 0, DT, true, false, true>),  \
+      reinterpret_cast<const void*>(grouped_gemm_fast_kernel<0, 0, DT, true, false, true>),  \
+      reinterpret_cast<const void*>(grouped_gemm_fast_kernel<0, 0, DT, false, true, true>)
   const void* kernels[] = {PPMOE_KERNELS(MOE_BF16, false), PPMOE_KERNELS(MOE_BF16, true),
                            PPMOE_KERNELS(MOE_F16, false), PPMOE_KERNELS(MOE_F16, true),
                            reinterpret_cast<const void*>(grouped_gemm_fast_kernel<2, 0, MOE_BF16, false, false>),
                            reinterpret_cast<const void*>(grouped_gemm_fast_kernel<2, 0, MOE_F16, false, false>),
                            reinterpret_cast<const void*>(grouped_gemm_fast_kernel<0, 0, MOE_BF16, false, true>),
-                           reinterpret_cast<const void*>(grouped_gemm_fast_kernel<0, 0, MOE_F16, false, true>)};
+                           reinterpret_cast<const void*>(grouped_gemm_fast_kernel<0, 0, MOE_F16, false, true>),
+                           PPMOE_ADAPTED(MOE_BF16), PPMOE_ADAPTED(MOE_F16)};
+#undef PPMOE_ADAPTED
 #undef PPMOE_KERNELS
   for (const void* k : kernels) {
     hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
@@ -1100,7 +1115,8 @@ hipError_t launch_grouped_gemm_fast(int in_dtype, bool gelu, const bf16_t* A, co
                                     const int32_t* offsets, int n_exp, int few_most, int Nout,
                                     int K, void* workspace, hipStream_t s, int fuse,
                                     const int32_t* aux_rows, const float* aux_w, int aux_div,
-                                    const int32_t* aux_inv, bf16_t* C2, bool b_by_rows, int pick_cus) {
+                                    const int32_t* aux_inv, bf16_t* C2, bool b_by_rows, int pick_cus,
+                                    const AdapterRows* adapters) {
   using namespace fast;
   int blocks = 0, same_l2 = 0;
   hipError_t e = set_up_for_launch(s, &blocks, &same_l2);
@@ -1121,12 +1137,14 @@ hipError_t launch_grouped_gemm_fast(int in_dtype, bool gelu, const bf16_t* A, co
   // the rows it cannot place)
   if ((fuse == 1 && !gelu) || (fuse == 2 && gelu) || fuse < 0 || fuse > 2 ||
       (fuse != 0 && aux_rows == nullptr) || (fuse == 2 && aux_w == nullptr) || aux_div < 1 ||
-      (fuse == 2 && aux_div != 1 && (aux_inv == nullptr || C2 == nullptr)))
+      (fuse == 2 && aux_div != 1 && (aux_inv == nullptr || C2 == nullptr)) ||
+      (adapters != nullptr && (fuse != 0 || C2 != nullptr)))
     return hipErrorInvalidValue;
+  const AdapterRows rows = adapters != nullptr ? *adapters : AdapterRows{};
 #define PPMOE_LAUNCH_KERNEL(...)                                                      \
   __VA_ARGS__<<<blocks, kThreads, kLdsBytes, s>>>(     \
       A, B, C, offsets, n_exp, few_most, Nout, K, slots, flags, epoch, same_l2, spin_limit, aux_rows, aux_w, aux_div, \
-      aux_inv, C2, pick_cus)
+      aux_inv, C2, pick_cus, rows)
 #define PPMOE_LAUNCH_DT(G, F, DT, R) PPMOE_LAUNCH_KERNEL(grouped_gemm_fast_kernel<G, F, DT, R, false>)
 #define PPMOE_LAUNCH(G, F)                            \
   do {                                                \
@@ -1135,8 +1153,19 @@ hipError_t launch_grouped_gemm_fast(int in_dtype, bool gelu, const bf16_t* A, co
     else if (ragged) PPMOE_LAUNCH_DT(G, F, MOE_BF16, true);                  \
     else PPMOE_LAUNCH_DT(G, F, MOE_BF16, false);                             \
   } while (0)
-  if (b_by_rows) {
-    if (gelu || fuse != 0 || ragged) return hipErrorInvalidValue;
+#define PPMOE_LAUNCH_ADAPTED(DT)                                                                                  \
+  do {                                                                                                            \
+    if (b_by_rows) PPMOE_LAUNCH_KERNEL(grouped_gemm_fast_kernel<0, 0, DT, false, true, true>);                    \
+    else if (gelu && ragged) PPMOE_LAUNCH_KERNEL(grouped_gemm_fast_kernel<1, 0, DT, true, false, true>);          \
+    else if (gelu) PPMOE_LAUNCH_KERNEL(grouped_gemm_fast_kernel<1, 0, DT, false, false, true>);                   \
+    else if (ragged) PPMOE_LAUNCH_KERNEL(grouped_gemm_fast_kernel<0, 0, DT, true, false, true>);                  \
+    else PPMOE_LAUNCH_KERNEL(grouped_gemm_fast_kernel<0, 0, DT, false, false, true>);                             \
+  } while (0)
+  if (b_by_rows && (gelu || fuse != 0 || ragged)) return hipErrorInvalidValue;
+  if (adapters != nullptr) {
+    if (in_dtype == MOE_F16) PPMOE_LAUNCH_ADAPTED(MOE_F16);
+    else PPMOE_LAUNCH_ADAPTED(MOE_BF16);
+  } else if (b_by_rows) {
     if (in_dtype == MOE_F16) PPMOE_LAUNCH_KERNEL(grouped_gemm_fast_kernel<0, 0, MOE_F16, false, true>);
     else PPMOE_LAUNCH_KERNEL(grouped_gemm_fast_kernel<0, 0, MOE_BF16, false, true>);
   } else if (fuse == 1) PPMOE_LAUNCH(1, 1);
@@ -1147,6 +1176,7 @@ hipError_t launch_grouped_gemm_fast(int in_dtype, bool gelu, const bf16_t* A, co
     else PPMOE_LAUNCH_KERNEL(grouped_gemm_fast_kernel<2, 0, MOE_BF16, false, false>);
   } else if (gelu) PPMOE_LAUNCH(1, 0);
   else PPMOE_LAUNCH(0, 0);
+#undef PPMOE_LAUNCH_ADAPTED
 #undef PPMOE_LAUNCH_DT
 #undef PPMOE_LAUNCH_KERNEL
 #undef PPMOE_LAUNCH

@@ -34,12 +34,13 @@ constexpr int kLd = BN + 4;      // floats per row of partial sums in LDS
 // aux_rows[r] / aux_div of the matrix given as A.  2: packed row r belongs to assignment a = aux_rows[r] of
 // token a / aux_div; if it is that token's only kept pick here it is stored, times aux_w[a], as row `token`
 // of C, else unweighted as packed row r of C2.
-template <bool GELU, int FUSE, int DT>
+// ADAPT: the rows' adapters are added to the sums (a thread has four columns of one row: it reads four rows of `up` and one of `low`).
+template <bool GELU, int FUSE, int DT, bool ADAPT>
 __global__ __launch_bounds__(kThreads, 4) void grouped_gemm_few_rows_kernel(
     const bf16_t* __restrict__ A, const bf16_t* __restrict__ B, bf16_t* __restrict__ C,
     const int32_t* __restrict__ offsets, int n_exp, int Nout, int K, int most, const int32_t* __restrict__ aux_rows,
     const float* __restrict__ aux_w, int aux_div, const int32_t* __restrict__ aux_inv, bf16_t* __restrict__ C2,
-    unsigned long long* __restrict__ clock_words) {
+    unsigned long long* __restrict__ clock_words, AdapterRows adapters) {
   typedef typename Elem16<DT>::vec8 vec8;
   __shared__ __attribute__((aligned(16))) float part[kWaves][kTok][kLd];
   if (most > 0 && !no_expert_above(offsets, n_exp, most)) return;
@@ -62,6 +63,32 @@ __global__ __launch_bounds__(kThreads, 4) void grouped_gemm_few_rows_kernel(
 
   // Finishes four columns of packed row `row`.
   auto store = [&](int row, int n, f32x4 v) __attribute__((always_inline)) {
+    if constexpr (ADAPT) {
+      const int a = adapters.of_row[row];
+      if (a >= 0) {
+        const u32x4* low = reinterpret_cast<const u32x4*>(adapters.low + static_cast<int64_t>(row) * adapters.rank);
+        const u32x4* up = reinterpret_cast<const u32x4*>(
+            adapters.up + ((static_cast<int64_t>(a) * adapters.n_exp + expert) * Nout + col0 + n) * adapters.rank);
+        const int pieces = adapters.rank >> 3;
+        f32x4 more = {0.f, 0.f, 0.f, 0.f};
+#pragma clang loop unroll(disable)
+        for (int p = 0; p < pieces; ++p) {
+          const u32x4 l = low[p];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const u32x4 u = up[i * pieces + p];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float l0, l1, u0, u1;
+              Elem16<DT>::widen2(l[q], l0, l1);
+              Elem16<DT>::widen2(u[q], u0, u1);
+              more[i] = fmaf(l1, u1, fmaf(l0, u0, more[i]));
+            }
+          }
+        }
+        v += more;
+      }
+    }
     if (GELU) v = gelu_tanh4(v);
     bf16_t* base = C;
     if (FUSE == 2) {
@@ -161,29 +188,32 @@ hipError_t launch_grouped_gemm_few_rows(int in_dtype, bool gelu, const bf16_t* A
                                         const int32_t* offsets, int n_exp, int Nout, int K, int most,
                                         void* workspace, hipStream_t s, int fuse,
                                         const int32_t* aux_rows, const float* aux_w, int aux_div,
-                                        const int32_t* aux_inv, bf16_t* C2) {
+                                        const int32_t* aux_inv, bf16_t* C2, const AdapterRows* adapters) {
   using namespace few;
   if ((fuse == 1 && !gelu) || (fuse == 2 && gelu) || fuse < 0 || fuse > 2 || (fuse != 0 && aux_rows == nullptr) ||
       (fuse == 2 && aux_w == nullptr) || aux_div < 1 ||
-      (fuse == 2 && aux_div != 1 && (aux_inv == nullptr || C2 == nullptr)))
+      (fuse == 2 && aux_div != 1 && (aux_inv == nullptr || C2 == nullptr)) || (fuse != 0 && adapters != nullptr))
     return hipErrorInvalidValue;
+  const AdapterRows rows = adapters != nullptr ? *adapters : AdapterRows{};
   const hipError_t e = grouped_gemm_set_up(s);
   if (e != hipSuccess) return e;
   unsigned long long* clock_words = gemm_clock_words(workspace);
   const unsigned grid = static_cast<unsigned>(n_exp) * static_cast<unsigned>((Nout + BN - 1) / BN);
-#define PPMOE_LAUNCH(G, F)                                                                                 \
+#define PPMOE_LAUNCH(G, F, ADAPT)                                                                          \
   do {                                                                                                     \
     if (in_dtype == MOE_F16)                                                                               \
-      grouped_gemm_few_rows_kernel<G, F, MOE_F16><<<grid, kThreads, 0, s>>>(                               \
-          A, B, C, offsets, n_exp, Nout, K, most, aux_rows, aux_w, aux_div, aux_inv, C2, clock_words);                  \
+      grouped_gemm_few_rows_kernel<G, F, MOE_F16, ADAPT><<<grid, kThreads, 0, s>>>(                        \
+          A, B, C, offsets, n_exp, Nout, K, most, aux_rows, aux_w, aux_div, aux_inv, C2, clock_words, rows);  \
     else                                                                                                   \
-      grouped_gemm_few_rows_kernel<G, F, MOE_BF16><<<grid, kThreads, 0, s>>>(                              \
-          A, B, C, offsets, n_exp, Nout, K, most, aux_rows, aux_w, aux_div, aux_inv, C2, clock_words);                  \
+      grouped_gemm_few_rows_kernel<G, F, MOE_BF16, ADAPT><<<grid, kThreads, 0, s>>>(                       \
+          A, B, C, offsets, n_exp, Nout, K, most, aux_rows, aux_w, aux_div, aux_inv, C2, clock_words, rows);  \
   } while (0)
-  if (fuse == 1) PPMOE_LAUNCH(true, 1);
-  else if (fuse == 2) PPMOE_LAUNCH(false, 2);
-  else if (gelu) PPMOE_LAUNCH(true, 0);
-  else PPMOE_LAUNCH(false, 0);
+  if (fuse == 1) PPMOE_LAUNCH(true, 1, false);
+  else if (fuse == 2) PPMOE_LAUNCH(false, 2, false);
+  else if (gelu && adapters != nullptr) PPMOE_LAUNCH(true, 0, true);
+  else if (gelu) PPMOE_LAUNCH(true, 0, false);
+  else if (adapters != nullptr) PPMOE_LAUNCH(false, 0, true);
+  else PPMOE_LAUNCH(false, 0, false);
 #undef PPMOE_LAUNCH
   return hipGetLastError();
 }
