@@ -9,6 +9,7 @@
 // kernels add the low-rank part to their accumulators (adapter_core.h), so y and dx are rounded once.  Here are the
 // products that are narrow in one direction: they read x or dy once and are bound by that.
 
+#include <atomic>
 #include <cmath>
 
 #include "adapter_core.h"
@@ -22,11 +23,14 @@ constexpr int kMaxColumns = 1 << 20;
 
 // ---- x A^T: [rows, K] with a matrix [rank, K] of each row's own ------------------------------------------
 //
-// A block has up to 16 packed rows, its wavefronts split the contraction, fetch both operands of the matrix instruction
-// from memory and meet in LDS, where the partial sums are added in wavefront order.  It goes through the distinct
-// (adapter, expert) pairs of its rows; each takes the whole contraction and is kept for the rows it belongs to (a row of the
-// operand never meets another one's).
-
+// A block has up to 16 G packed rows, its wavefronts split the contraction, fetch both operands of the matrix instruction
+// from memory and meet in LDS, where the partial sums are added in wavefront order.  Within a stretch of the contraction it goes through the
+// distinct (adapter, expert) pairs of its rows; a product is kept for the rows of its pair (a row of the operand never meets another
+// one's).  Consecutive blocks' rows mostly have the same pairs: an XCD takes a run of them, so that its L2 holds their matrices.
+//
+// What bounds it is what a CU fetches, x and the pairs' matrices: (16 G + rank) K elements per block of one pair.  Ranks
+// above 32 take 64 rows a block, and where that leaves CUs without one the contraction is cut between blocks as well, whose partial sums
+// another launch adds (combine_kernel).
 struct ShrinkArgs {
   const bf16_t* x;        // [rows, K]
   const bf16_t* m;        // [n_adapters, n_exp, rank, K]
@@ -37,91 +41,156 @@ struct ShrinkArgs {
   bf16_t* low;            // out [rows, rank]: scaled, in 16 bits
   int n_exp, n_adapters, top_k, K, rank, tile_rows;
   bool scale_wide;        // wide is scaled as well
+  int32_t* ticket;        // of count_kernel, set to 0; or NULL
+  float* partial;         // [cuts, rows, rank] or NULL
+  int cuts, rows;
 };
 
-template <int DT, int MR, int WAVES>   // MR: blocks of 16 of the rank
+// (low in 16 bits: an operand of the matrix instruction that adds the low-rank part.  A rounding of each of `rank` terms, as
+// far off as the one rounding of the result is, and only of the low-rank part.)
+template <int DT>
+__device__ __forceinline__ void store_low_rank(const ShrinkArgs& a, int64_t at, f32x4 v, float scale) {
+  const f32x4 scaled = v * scale;
+  *reinterpret_cast<f32x4*>(a.wide + at) = a.scale_wide ? scaled : v;
+  const u32x2 o = {Elem16<DT>::pack2(scaled[0], scaled[1]), Elem16<DT>::pack2(scaled[2], scaled[3])};
+  *reinterpret_cast<u32x2*>(a.low + at) = o;
+}
+
+// MR: blocks of 16 of the rank; J: k-steps of 32 fetched at a time
+template <int DT, int MR, int WAVES, int G, int J>
 __global__ __launch_bounds__(64 * WAVES) void shrink_kernel(ShrinkArgs a) {
   typedef typename Elem16<DT>::vec8 vec8;
-  __shared__ __attribute__((aligned(16))) float part[WAVES][16][16 * MR + 4];
+  extern __shared__ __attribute__((aligned(16))) float shrink_lds[];
+  auto part = reinterpret_cast<float(*)[16 * G][16 * MR + 4]>(shrink_lds);   // [WAVES]
+  __shared__ float row_scale[16 * G];
+  __shared__ int row_pair[16 * G];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 15, fq = lane >> 4;
+  if (a.ticket != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
   const int lo = a.offsets[0], rows = a.offsets[a.n_exp] - lo;
-  const int row0 = blockIdx.x * a.tile_rows;
+  const int per = gridDim.x >> 3, nth = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  const int tile = nth / a.cuts, cut = nth - tile * a.cuts;
+  const int row0 = tile * a.tile_rows;
   const int count = min(a.tile_rows, rows - row0);
   if (count <= 0) return;
-  // this lane's row: its expert (the experts whose rows end at or before it), its adapter
-  const int r = lo + row0 + min(fr, count - 1);
-  int expert = 0;
-  for (int i0 = 0; i0 < a.n_exp; i0 += 64) {
-    const int end = a.offsets[min(i0 + lane, a.n_exp - 1) + 1];
-    for (int q = 0; q < 16; ++q) {
-      const int n = __popcll(__ballot(i0 + lane < a.n_exp && end <= __builtin_amdgcn_readlane(r, q)));
-      if (fr == q) expert += n;
-    }
-  }
-  int id = a.adapter[a.perm != nullptr ? a.perm[r] / a.top_k : r];
-  if (id < 0 || id >= a.n_adapters) id = -1;
-  if (wave == 0 && lane < count) a.of_row[r] = id;
-  const int mine = id >= 0 && fr < count ? id * a.n_exp + expert : -1;
-
+  // the contraction's share of this block, in whole stretches of all its wavefronts
+  constexpr int kStretch = WAVES * 32 * J;
+  const int stretches = (a.K + kStretch - 1) / kStretch;
+  const int k_end = min(a.K, (cut + 1) * stretches / a.cuts * kStretch), k_begin = cut * stretches / a.cuts * kStretch;
+  int r[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) r[g] = lo + row0 + min(g * 16 + fr, count - 1);
   const u32x4 zero = u32x4{0u, 0u, 0u, 0u};
-  f32x4 kept[MR];
+  u32x4 x[J][G];
+  auto load_x = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
-  for (int mr = 0; mr < MR; ++mr) kept[mr] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const bf16_t* xr = a.x + static_cast<int64_t>(r) * a.K + fq * 8;
-  int pair = -1;
-  while (true) {
-    int least = mine > pair ? mine : 0x7fffffff;
+    for (int j = 0; j < J; ++j)
 #pragma unroll
-    for (int off = 8; off >= 1; off >>= 1) least = min(least, __shfl_xor(least, off, 64));
-    pair = __builtin_amdgcn_readfirstlane(least);
-    if (pair == 0x7fffffff) break;
-    const bf16_t* m = a.m + static_cast<int64_t>(pair) * a.rank * a.K + fq * 8;
-    f32x4 acc[MR];
+      for (int g = 0; g < G; ++g)
+        x[j][g] = k0 + 32 * j + fq * 8 < k_end ? *reinterpret_cast<const u32x4*>(a.x + static_cast<int64_t>(r[g]) * a.K + k0 + 32 * j + fq * 8) : zero;
+  };
+  int k0 = k_begin + wave * 32 * J;
+  load_x(k0);   // (on their way while the pairs are looked up)
+  if (wave == 0 && lane < 16 * G) {
+    const bool is = lane < count;
+    const int row = lo + row0 + min(lane, count - 1);
+    int id = a.adapter[a.perm != nullptr ? a.perm[row] / a.top_k : row];
+    if (id < 0 || id >= a.n_adapters) id = -1;
+    int expert = 0;   // how many experts' rows end at or before this one
+    for (int i = 1; i < a.n_exp; ++i) expert += a.offsets[i] <= row;
+    if (is && cut == 0) a.of_row[row] = id;
+    row_scale[lane] = id >= 0 && a.scale != nullptr ? a.scale[id] : 1.f;
+    row_pair[lane] = id >= 0 && is ? id * a.n_exp + expert : -1;
+  }
+  __syncthreads();
+  int mine[G];
 #pragma unroll
-    for (int mr = 0; mr < MR; ++mr) acc[mr] = f32x4{0.f, 0.f, 0.f, 0.f};
-    constexpr int J = MR <= 2 ? 4 : 2;   // k-steps of 32 fetched at a time
-    for (int k0 = wave * 32 * J; k0 < a.K; k0 += WAVES * 32 * J) {
-      u32x4 x[J], w[J][MR];
+  for (int g = 0; g < G; ++g) mine[g] = row_pair[g * 16 + fr];
+
+  f32x4 acc[G][MR];
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const int k = k0 + 32 * j;
-        const bool ok = k + fq * 8 < a.K;
-        x[j] = ok ? *reinterpret_cast<const u32x4*>(xr + k) : zero;
+  for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int mr = 0; mr < MR; ++mr)   // (rows past the rank re-read the last one; their sums are not stored)
-          w[j][mr] = ok ? *reinterpret_cast<const u32x4*>(m + static_cast<int64_t>(min(mr * 16 + fr, a.rank - 1)) * a.K + k) : zero;
-      }
-      __builtin_amdgcn_sched_barrier(0);
+    for (int mr = 0; mr < MR; ++mr) acc[g][mr] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int first = __builtin_amdgcn_readfirstlane(least_above(mine, -1));
+  // (the next pair's, or stretch's, operand is on its way while this one's is multiplied)
+  auto load_w = [&](u32x4 (&w)[J][MR], int pair, int k) __attribute__((always_inline)) {
+    const bf16_t* m = a.m + static_cast<int64_t>(pair) * a.rank * a.K + k + fq * 8;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int mr = 0; mr < MR; ++mr)   // (rows past the rank re-read the last one; their sums are not stored)
+        w[j][mr] = k + 32 * j + fq * 8 < k_end
+                       ? *reinterpret_cast<const u32x4*>(m + static_cast<int64_t>(min(mr * 16 + fr, a.rank - 1)) * a.K + 32 * j)
+                       : zero;
+  };
+  auto multiply = [&](const u32x4 (&w)[J][MR], int pair) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      f32x4 sum[MR];
+#pragma unroll
+      for (int mr = 0; mr < MR; ++mr) sum[mr] = acc[g][mr];
 #pragma unroll
       for (int j = 0; j < J; ++j)
 #pragma unroll
         for (int mr = 0; mr < MR; ++mr)
-          acc[mr] = Elem16<DT>::mfma16(__builtin_bit_cast(vec8, w[j][mr]), __builtin_bit_cast(vec8, x[j]), acc[mr]);
-    }
-    // D: lane row fr, rank index mr * 16 + fq * 4 + v
+          sum[mr] = Elem16<DT>::mfma16(__builtin_bit_cast(vec8, w[j][mr]), __builtin_bit_cast(vec8, x[j][g]), sum[mr]);
+      // D: lane row fr, rank index mr * 16 + fq * 4 + v
 #pragma unroll
-    for (int mr = 0; mr < MR; ++mr)
-      if (mine == pair) kept[mr] = acc[mr];
+      for (int mr = 0; mr < MR; ++mr)
+        if (mine[g] == pair) acc[g][mr] = sum[mr];
+    }
+  };
+  if (first != kNone && k0 < k_end) {
+    u32x4 w0[J][MR], w1[J][MR];
+    int pair = first, now;
+    load_w(w0, pair, k0);
+    // what follows (pair, k0): the next pair of the same stretch, or the first one of the next
+    auto turn = [&](u32x4 (&w)[J][MR], u32x4 (&other)[J][MR]) __attribute__((always_inline)) -> bool {
+      now = pair;
+      pair = __builtin_amdgcn_readfirstlane(least_above(mine, pair));
+      const bool same = pair != kNone;
+      if (!same) {
+        pair = first;
+        k0 += kStretch;
+      }
+      const bool more = k0 < k_end;
+      if (more) load_w(other, pair, k0);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(w, now);
+      if (more && !same) load_x(k0);
+      return more;
+    };
+    while (turn(w0, w1) && turn(w1, w0)) {
+    }
   }
 #pragma unroll
-  for (int mr = 0; mr < MR; ++mr) *reinterpret_cast<f32x4*>(&part[wave][fr][mr * 16 + fq * 4]) = kept[mr];
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int mr = 0; mr < MR; ++mr) *reinterpret_cast<f32x4*>(&part[wave][g * 16 + fr][mr * 16 + fq * 4]) = acc[g][mr];
   __syncthreads();
   for (int p = threadIdx.x; p < count * (a.rank / 4); p += 64 * WAVES) {
     const int q = p / (a.rank / 4), j = (p - q * (a.rank / 4)) * 4;
     f32x4 v = *reinterpret_cast<const f32x4*>(&part[0][q][j]);
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) v += *reinterpret_cast<const f32x4*>(&part[w][q][j]);
-    const int row = lo + row0 + q;
-    int whose = a.adapter[a.perm != nullptr ? a.perm[row] / a.top_k : row];
-    if (whose < 0 || whose >= a.n_adapters) whose = -1;
-    const float s = whose < 0 || a.scale == nullptr ? 1.f : a.scale[whose];
-    const f32x4 scaled = v * s;
-    *reinterpret_cast<f32x4*>(a.wide + static_cast<int64_t>(row) * a.rank + j) = a.scale_wide ? scaled : v;
-    // (16 bits: an operand of the matrix instruction that adds the low-rank part.  A rounding of each of `rank` terms, as
-    // far off as the one rounding of the result is, and only of the low-rank part.)
-    const u32x2 o = {Elem16<DT>::pack2(scaled[0], scaled[1]), Elem16<DT>::pack2(scaled[2], scaled[3])};
-    *reinterpret_cast<u32x2*>(a.low + static_cast<int64_t>(row) * a.rank + j) = o;
+    const int64_t at = static_cast<int64_t>(lo + row0 + q) * a.rank + j;
+    if (a.cuts > 1) *reinterpret_cast<f32x4*>(a.partial + cut * static_cast<int64_t>(a.rows) * a.rank + at) = v;
+    else store_low_rank<DT>(a, at, v, row_scale[q]);
+  }
+}
+
+// The shares of a cut contraction, added in order.
+template <int DT>
+__global__ __launch_bounds__(256) void combine_kernel(ShrinkArgs a) {
+  const int lo = a.offsets[0], quads = a.rank / 4;
+  const int64_t total = static_cast<int64_t>(a.offsets[a.n_exp] - lo) * quads;
+  for (int64_t p = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; p < total; p += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t row = lo + p / quads, at = row * a.rank + (p % quads) * 4;
+    f32x4 v = *reinterpret_cast<const f32x4*>(a.partial + at);
+    for (int cut = 1; cut < a.cuts; ++cut) v += *reinterpret_cast<const f32x4*>(a.partial + cut * static_cast<int64_t>(a.rows) * a.rank + at);
+    const int id = a.of_row[row];
+    store_low_rank<DT>(a, at, v, id >= 0 && a.scale != nullptr ? a.scale[id] : 1.f);
   }
 }
 
@@ -160,14 +229,19 @@ __global__ __launch_bounds__(256) void transpose_kernel(const bf16_t* __restrict
 // ---- the rows of each (adapter, expert) pair -----------------------------------------------------------
 //
 // list: the packed rows ordered by pair (adapter-major, as dA and dB are), ascending inside it; begin[pair] where they start.
-// A pair's rows are cut into pieces of at most `most` for the gradients; a pair of several pieces has a slot of partial sums
-// for each.  Counted, scanned, filled: no atomics, the same order on every run.
+// A pair's rows are cut into pieces of at most `most` for a gradient (one table for dA, one for dB); a pair of several pieces
+// has a slot of partial sums for each.  Counted, scanned, filled: the same order on every run.
+struct Pieces {
+  int32_t *begin;   // [pairs + 1] first piece of a pair
+  int32_t *slot;    // [pairs + 1] its first slot
+  int32_t *pair;    // [most pieces] a piece's pair
+  int most;
+};
 struct Groups {
-  int32_t *begin;         // [pairs + 1]
-  int32_t *piece_begin;   // [pairs + 1]
-  int32_t *slot_begin;    // [pairs + 1]
-  int32_t *piece_pair;    // [most pieces]
-  int32_t *list;          // [rows]
+  int32_t *begin;   // [pairs + 1]
+  int32_t *list;    // [rows]
+  int32_t *ticket;  // blocks of count_kernel that are done
+  Pieces pieces[2];
 };
 
 __device__ __forceinline__ int sum_of_block(int v, int* lds) {   // 256 threads
@@ -179,28 +253,33 @@ __device__ __forceinline__ int sum_of_block(int v, int* lds) {   // 256 threads
   return lds[0] + lds[1] + lds[2] + lds[3];
 }
 
-__global__ __launch_bounds__(256) void count_kernel(const int32_t* __restrict__ of_row, const int32_t* __restrict__ offsets, int n_exp,
-                                                    int32_t* __restrict__ count) {
+// A block counts a pair's rows; the one that comes last adds them up (the ticket: which one that is does not show in what it writes).
+__global__ __launch_bounds__(256) void count_kernel(const int32_t* __restrict__ of_row, const int32_t* __restrict__ offsets, int n_exp, Groups g,
+                                                    int pairs) {
   __shared__ int lds[4];
-  const int id = blockIdx.x / n_exp, expert = blockIdx.x - id * n_exp;
-  int n = 0;
-  for (int r = offsets[expert] + threadIdx.x; r < offsets[expert + 1]; r += 256) n += of_row[r] == id;
-  n = sum_of_block(n, lds);
-  if (threadIdx.x == 0) count[blockIdx.x] = n;
-}
-
-// One block of 1024 threads; count[] is begin[] (overwritten).
-__global__ __launch_bounds__(1024) void scan_kernel(Groups g, int pairs, int most) {
-  __shared__ int sums[3][16];
-  int before[3] = {0, 0, 0};
+  __shared__ int last;
+  __shared__ int sums[5][4];
+  {
+    const int id = blockIdx.x / n_exp, expert = blockIdx.x - id * n_exp;
+    int n = 0;
+    for (int r = offsets[expert] + threadIdx.x; r < offsets[expert + 1]; r += 256) n += of_row[r] == id;
+    n = sum_of_block(n, lds);
+    if (threadIdx.x == 0) {
+      __hip_atomic_store(g.begin + blockIdx.x, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      last = __hip_atomic_fetch_add(g.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == pairs - 1;
+    }
+  }
+  __syncthreads();
+  if (!last) return;
+  int before[5] = {0, 0, 0, 0, 0};
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int p0 = 0; p0 < pairs; p0 += 1024) {
+  for (int p0 = 0; p0 < pairs; p0 += 256) {
     const int p = p0 + threadIdx.x;
-    const int n = p < pairs ? g.begin[p] : 0;
-    const int pieces = (n + most - 1) / most;
-    int own[3] = {n, pieces, pieces > 1 ? pieces : 0}, up_to[3];
+    const int n = p < pairs ? __hip_atomic_load(g.begin + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+    const int p_a = (n + g.pieces[0].most - 1) / g.pieces[0].most, p_b = (n + g.pieces[1].most - 1) / g.pieces[1].most;
+    int own[5] = {n, p_a, p_a > 1 ? p_a : 0, p_b, p_b > 1 ? p_b : 0}, up_to[5];
 #pragma unroll
-    for (int q = 0; q < 3; ++q) {
+    for (int q = 0; q < 5; ++q) {
       int v = own[q];
 #pragma unroll
       for (int off = 1; off < 64; off <<= 1) {
@@ -211,12 +290,13 @@ __global__ __launch_bounds__(1024) void scan_kernel(Groups g, int pairs, int mos
       if (lane == 63) sums[q][wave] = v;
     }
     __syncthreads();
-    int total[3];
+    int total[5];
 #pragma unroll
-    for (int q = 0; q < 3; ++q) {
+    for (int q = 0; q < 5; ++q) {
       int base = 0;
       total[q] = 0;
-      for (int w = 0; w < 16; ++w) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
         if (w < wave) base += sums[q][w];
         total[q] += sums[q][w];
       }
@@ -224,17 +304,21 @@ __global__ __launch_bounds__(1024) void scan_kernel(Groups g, int pairs, int mos
     }
     if (p < pairs) {
       g.begin[p] = up_to[0];
-      g.piece_begin[p] = up_to[1];
-      g.slot_begin[p] = up_to[2];
+      g.pieces[0].begin[p] = up_to[1];
+      g.pieces[0].slot[p] = up_to[2];
+      g.pieces[1].begin[p] = up_to[3];
+      g.pieces[1].slot[p] = up_to[4];
     }
 #pragma unroll
-    for (int q = 0; q < 3; ++q) before[q] += total[q];
+    for (int q = 0; q < 5; ++q) before[q] += total[q];
     __syncthreads();
   }
   if (threadIdx.x == 0) {
     g.begin[pairs] = before[0];
-    g.piece_begin[pairs] = before[1];
-    g.slot_begin[pairs] = before[2];
+    g.pieces[0].begin[pairs] = before[1];
+    g.pieces[0].slot[pairs] = before[2];
+    g.pieces[1].begin[pairs] = before[3];
+    g.pieces[1].slot[pairs] = before[4];
   }
 }
 
@@ -244,8 +328,11 @@ __global__ __launch_bounds__(256) void fill_kernel(const int32_t* __restrict__ o
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int at = g.begin[pair];
   if (at == g.begin[pair + 1]) return;
-  const int p0 = g.piece_begin[pair], p1 = g.piece_begin[pair + 1];
-  for (int p = p0 + threadIdx.x; p < p1; p += 256) g.piece_pair[p] = pair;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int p0 = g.pieces[t].begin[pair], p1 = g.pieces[t].begin[pair + 1];
+    for (int p = p0 + threadIdx.x; p < p1; p += 256) g.pieces[t].pair[p] = pair;
+  }
   const int end = offsets[expert + 1];
   for (int r0 = offsets[expert]; r0 < end; r0 += 256) {
     const int r = r0 + threadIdx.x;
@@ -263,47 +350,51 @@ __global__ __launch_bounds__(256) void fill_kernel(const int32_t* __restrict__ o
 
 // ---- G[pair][j, c] = sum over the pair's rows of s u[r, j] z[r, c] ------------------------------------------
 //
-// u [rows, rank] float32 (t, or v), z [rows, C] 16-bit (x, or dy).  BY_COLUMN: stored [C, rank] (dB), else [rank, C] (dA).
-// A block takes one piece of a pair's rows and 256 columns, 32 rows at a time: z as it is into LDS and from there
-// across its rows into operands (transposing read), u as two 16-bit summands (what the first one's rounding leaves, rounded
-// again: 16 or 22 bits together), so that the products keep float32's accuracy as far as the result shows it.  fp16: u is first brought
+// u [rows, rank] float32 (t, or v), z [rows, C] 16-bit (x, or dy).  dA is stored [rank, C], dB [C, rank] (BY_COLUMN).
+// A block takes one piece of a pair's rows and 128 columns, 64 rows at a time: z as it is into LDS and from there
+// across its rows into operands (transposing read), u as 16-bit summands, each the rounding of what those before it leave: three for
+// bf16, two for fp16 (24 and 22 bits together), so that the result has float32's accuracy.  fp16: u is first brought
 // to a largest value of 2^13 by a power of two, exactly, as its small values have no 22 bits.
-constexpr int kGradColumns = 256, kGradThreads = 256, kGradRows = 32;
-constexpr int kLowStride = kGradRows * 2 + 16;   // bytes of a row of u's halves in LDS
+constexpr int kGradColumns = 128, kGradThreads = 256, kGradRows = 64;
+constexpr int kLowStride = kGradRows * 2 + 16;   // bytes of a row of u's summands in LDS
 
 struct GradArgs {
   const float* u;
   const float* scale;           // by adapter, or NULL
   const bf16_t* z;
   float *out, *partial;         // [pairs, rank * C], [slots, rank * C]
+  Pieces pieces;
+  int C;
+};
+struct BothGrads {
+  GradArgs of[2];               // dA, dB
   Groups g;
-  int pairs, n_exp, rank, C, most;
+  int pairs, n_exp, rank, blocks_a;
 };
 
 template <int DT, int MR, bool BY_COLUMN>
-__global__ __launch_bounds__(kGradThreads) void gradient_kernel(GradArgs a) {
+__device__ __forceinline__ void gradient_piece(const BothGrads& b, const GradArgs& a, int block, unsigned char* z_lds, unsigned char* u_lds,
+                                               float* wave_top) {
   typedef typename Elem16<DT>::vec8 vec8;
-  __shared__ __attribute__((aligned(16))) unsigned char z_lds[kGradRows * kGradColumns * 2];
-  __shared__ __attribute__((aligned(16))) unsigned char u_lds[2][16 * MR * kLowStride];
-  __shared__ float wave_top[4];
+  constexpr int P = DT == MOE_F16 ? 2 : 3;   // summands
   const int col_blocks = (a.C + kGradColumns - 1) / kGradColumns;
-  const int piece = blockIdx.x / col_blocks, col0 = (blockIdx.x - piece * col_blocks) * kGradColumns;
-  if (piece >= a.g.piece_begin[a.pairs]) return;
-  const int pair = a.g.piece_pair[piece];
-  const int nth = piece - a.g.piece_begin[pair], pieces = a.g.piece_begin[pair + 1] - a.g.piece_begin[pair];
-  const int first = a.g.begin[pair] + nth * a.most, count = min(a.most, a.g.begin[pair + 1] - first);
-  const int32_t* list = a.g.list + first;
+  const int piece = block / col_blocks, col0 = (block - piece * col_blocks) * kGradColumns;
+  if (piece >= a.pieces.begin[b.pairs]) return;
+  const int pair = a.pieces.pair[piece];
+  const int nth = piece - a.pieces.begin[pair], pieces = a.pieces.begin[pair + 1] - a.pieces.begin[pair];
+  const int first = b.g.begin[pair] + nth * a.pieces.most, count = min(a.pieces.most, b.g.begin[pair + 1] - first);
+  const int32_t* list = b.g.list + first;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int fr = lane & 15, fq = lane >> 4;
-  const float s = a.scale != nullptr ? a.scale[pair / a.n_exp] : 1.f;
-  const int quads = a.rank / 4;   // of a row of u
+  const float s = a.scale != nullptr ? a.scale[pair / b.n_exp] : 1.f;
+  const int rank = b.rank, quads = rank / 4;   // of a row of u
 
   float up = 1.f, down = 1.f;
   if (DT == MOE_F16) {
     float top = 0.f;
     for (int p = tid; p < count * quads; p += kGradThreads) {
       const int q = p / quads;
-      const f32x4 v = *reinterpret_cast<const f32x4*>(a.u + static_cast<int64_t>(list[q]) * a.rank + (p - q * quads) * 4);
+      const f32x4 v = *reinterpret_cast<const f32x4*>(a.u + static_cast<int64_t>(list[q]) * rank + (p - q * quads) * 4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(v[e] * s));
     }
@@ -319,116 +410,141 @@ __global__ __launch_bounds__(kGradThreads) void gradient_kernel(GradArgs a) {
     }
   }
 
-  // staging: z in 1024 pieces of 16 bytes, four per thread (row p / 32, piece p % 32); u in quads
+  // staging: z in 1024 pieces of 16 bytes, four per thread (row p / 16, piece p % 16); u in quads
   u32x4 zv[4];
-  constexpr int kQuads = (16 * MR * kGradRows / 4 + kGradThreads - 1) / kGradThreads;
+  constexpr int kQuads = 16 * MR * kGradRows / 4 / kGradThreads;
   f32x4 uv[kQuads];
   auto load = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int p = tid + i * kGradThreads, row = k0 + (p >> 5), c = col0 + (p & 31) * 8;
+      const int p = tid + i * kGradThreads, row = k0 + (p >> 4), c = col0 + (p & 15) * 8;
       zv[i] = row < count && c < a.C ? *reinterpret_cast<const u32x4*>(a.z + static_cast<int64_t>(list[row]) * a.C + c) : u32x4{0u, 0u, 0u, 0u};
     }
 #pragma unroll
     for (int i = 0; i < kQuads; ++i) {
-      const int p = tid + i * kGradThreads, q = p & (kGradRows - 1), j = (p / kGradRows) * 4, row = k0 + q;
-      uv[i] = row < count && j < a.rank ? *reinterpret_cast<const f32x4*>(a.u + static_cast<int64_t>(list[row]) * a.rank + j) : f32x4{0.f, 0.f, 0.f, 0.f};
+      const int p = tid + i * kGradThreads, q = p / (4 * MR), j = (p % (4 * MR)) * 4, row = k0 + q;
+      uv[i] = row < count && j < rank ? *reinterpret_cast<const f32x4*>(a.u + static_cast<int64_t>(list[row]) * rank + j) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
   // 32-byte block b of row k at b ^ ((k & 3) + 4 ((k >> 3) & 1)): what 32 lanes of a transposing read touch falls on all banks
   auto store = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int p = tid + i * kGradThreads, k = p >> 5, c = p & 31;
-      const int block = (c >> 1) ^ ((k & 3) + 4 * ((k >> 3) & 1));
-      *reinterpret_cast<u32x4*>(z_lds + k * (kGradColumns * 2) + block * 32 + (c & 1) * 16) = zv[i];
+      const int p = tid + i * kGradThreads, k = p >> 4, c = p & 15;
+      const int blk = (c >> 1) ^ ((k & 3) + 4 * ((k >> 3) & 1));
+      *reinterpret_cast<u32x4*>(z_lds + k * (kGradColumns * 2) + blk * 32 + (c & 1) * 16) = zv[i];
     }
 #pragma unroll
     for (int i = 0; i < kQuads; ++i) {
-      const int p = tid + i * kGradThreads, q = p & (kGradRows - 1), j = (p / kGradRows) * 4;
-      if (j < 16 * MR) {
+      const int p = tid + i * kGradThreads, q = p / (4 * MR), j = (p % (4 * MR)) * 4;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float v = uv[i][e] * s * up;
-          const uint16_t hi = static_cast<uint16_t>(Elem16<DT>::pack2(v, 0.f));
-          const float rest = v - Elem16<DT>::widen(hi);
-          // (an infinite or NaN v: the rest is NaN or 0 * ..., and the sum is what it has to be with the rest left out)
-          const uint16_t lo = static_cast<uint16_t>(Elem16<DT>::pack2(fabsf(rest) < 3.0e38f ? rest : 0.f, 0.f));
-          *reinterpret_cast<uint16_t*>(u_lds[0] + (j + e) * kLowStride + q * 2) = hi;
-          *reinterpret_cast<uint16_t*>(u_lds[1] + (j + e) * kLowStride + q * 2) = lo;
+      for (int e = 0; e < 4; ++e) {
+        float rest = uv[i][e] * s * up;
+#pragma unroll
+        for (int part = 0; part < P; ++part) {
+          const uint16_t h = static_cast<uint16_t>(Elem16<DT>::pack2(rest, 0.f));
+          *reinterpret_cast<uint16_t*>(u_lds + part * (16 * MR * kLowStride) + (j + e) * kLowStride + q * 2) = h;
+          rest -= Elem16<DT>::widen(h);
+          if (!(fabsf(rest) < 3.0e38f)) rest = 0.f;   // (an infinity or a NaN is in the first summand whole)
         }
       }
     }
   };
 
-  f32x4 acc[MR][4];
+  f32x4 acc[MR][2];
 #pragma unroll
   for (int mr = 0; mr < MR; ++mr)
 #pragma unroll
-    for (int ni = 0; ni < 4; ++ni) acc[mr][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const uint32_t z0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) unsigned char*)z_lds));
+    for (int ni = 0; ni < 2; ++ni) acc[mr][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint32_t z0 = core::lds_address(z_lds);
   load(0);
   for (int k0 = 0; k0 < count; k0 += kGradRows) {
     __syncthreads();
     store();
     __syncthreads();
     if (k0 + kGradRows < count) load(k0 + kGradRows);
-    u32x2 zt[4][2];
     const int j = (lane >> 2) & 3;
 #pragma unroll
-    for (int ni = 0; ni < 4; ++ni) {
-      const uint32_t at = z0 + (fq * 8 + j) * (kGradColumns * 2) + (((wave * 4 + ni) ^ (j + 4 * (fq & 1))) << 5) + (lane & 3) * 8;
-      asm volatile("ds_read_b64_tr_b16 %0, %2\n\tds_read_b64_tr_b16 %1, %2 offset:2048"
-                   : "=&v"(zt[ni][0]), "=&v"(zt[ni][1]) : "v"(at) : "memory");
-    }
-    vec8 uh[MR], ul[MR];
+    for (int ks = 0; ks < kGradRows / 32; ++ks) {
+      u32x2 zt[2][2];
 #pragma unroll
-    for (int mr = 0; mr < MR; ++mr) {
-      uh[mr] = *reinterpret_cast<const vec8*>(u_lds[0] + (mr * 16 + fr) * kLowStride + fq * 16);
-      ul[mr] = *reinterpret_cast<const vec8*>(u_lds[1] + (mr * 16 + fr) * kLowStride + fq * 16);
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(zt[0][0]), "+v"(zt[0][1]), "+v"(zt[1][0]), "+v"(zt[1][1]), "+v"(zt[2][0]), "+v"(zt[2][1]),
-                 "+v"(zt[3][0]), "+v"(zt[3][1]) : : "memory");
+      for (int ni = 0; ni < 2; ++ni) {
+        const uint32_t at = z0 + (ks * 32 + fq * 8 + j) * (kGradColumns * 2) + (((wave * 2 + ni) ^ (j + 4 * (fq & 1))) << 5) + (lane & 3) * 8;
+        asm volatile("ds_read_b64_tr_b16 %0, %2\n\tds_read_b64_tr_b16 %1, %2 offset:1024"
+                     : "=&v"(zt[ni][0]), "=&v"(zt[ni][1]) : "v"(at) : "memory");
+      }
+      vec8 u[P][MR];
 #pragma unroll
-    for (int ni = 0; ni < 4; ++ni) {
-      const vec8 z = __builtin_bit_cast(vec8, __builtin_shufflevector(zt[ni][0], zt[ni][1], 0, 1, 2, 3));
+      for (int part = 0; part < P; ++part)
 #pragma unroll
-      for (int mr = 0; mr < MR; ++mr) {
-        // D: lane: index of the second operand, registers: 4 (lane / 16) + v of the first
-        if (BY_COLUMN) {
-          acc[mr][ni] = Elem16<DT>::mfma16(uh[mr], z, acc[mr][ni]);
-          acc[mr][ni] = Elem16<DT>::mfma16(ul[mr], z, acc[mr][ni]);
-        } else {
-          acc[mr][ni] = Elem16<DT>::mfma16(z, uh[mr], acc[mr][ni]);
-          acc[mr][ni] = Elem16<DT>::mfma16(z, ul[mr], acc[mr][ni]);
-        }
+        for (int mr = 0; mr < MR; ++mr)
+          u[part][mr] = *reinterpret_cast<const vec8*>(u_lds + part * (16 * MR * kLowStride) + (mr * 16 + fr) * kLowStride + ks * 64 + fq * 16);
+      asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(zt[0][0]), "+v"(zt[0][1]), "+v"(zt[1][0]), "+v"(zt[1][1]) : : "memory");
+#pragma unroll
+      for (int ni = 0; ni < 2; ++ni) {
+        const vec8 z = __builtin_bit_cast(vec8, __builtin_shufflevector(zt[ni][0], zt[ni][1], 0, 1, 2, 3));
+#pragma unroll
+        for (int mr = 0; mr < MR; ++mr)
+#pragma unroll
+          for (int part = P - 1; part >= 0; --part)   // D: lane: index of the second operand, registers: 4 (lane / 16) + v of the first
+            acc[mr][ni] = BY_COLUMN ? Elem16<DT>::mfma16(u[part][mr], z, acc[mr][ni]) : Elem16<DT>::mfma16(z, u[part][mr], acc[mr][ni]);
       }
     }
   }
-  const int64_t size = static_cast<int64_t>(a.rank) * a.C;
-  float* out = pieces > 1 ? a.partial + (a.g.slot_begin[pair] + nth) * size : a.out + pair * size;
+  const int64_t size = static_cast<int64_t>(rank) * a.C;
+  float* out = pieces > 1 ? a.partial + (a.pieces.slot[pair] + nth) * size : a.out + pair * size;
 #pragma unroll
-  for (int ni = 0; ni < 4; ++ni)
+  for (int ni = 0; ni < 2; ++ni)
 #pragma unroll
     for (int mr = 0; mr < MR; ++mr) {
-      const int c = col0 + wave * 64 + ni * 16 + (BY_COLUMN ? fr : fq * 4), jj = mr * 16 + (BY_COLUMN ? fq * 4 : fr);
-      if (c < a.C && jj < a.rank)
-        *reinterpret_cast<f32x4*>(out + (BY_COLUMN ? static_cast<int64_t>(c) * a.rank + jj : static_cast<int64_t>(jj) * a.C + c)) =
+      const int c = col0 + wave * 32 + ni * 16 + (BY_COLUMN ? fr : fq * 4), jj = mr * 16 + (BY_COLUMN ? fq * 4 : fr);
+      if (c < a.C && jj < rank)
+        *reinterpret_cast<f32x4*>(out + (BY_COLUMN ? static_cast<int64_t>(c) * rank + jj : static_cast<int64_t>(jj) * a.C + c)) =
             acc[mr][ni] * down;
     }
 }
 
-// Pairs without rows: zeros; of several pieces: the partial sums in order.
-__global__ __launch_bounds__(256) void finish_kernel(GradArgs a, int per_pair) {
-  const int pair = blockIdx.x / per_pair, part = blockIdx.x - pair * per_pair;
-  const int slot = a.g.slot_begin[pair], slots = a.g.slot_begin[pair + 1] - slot;
-  if (slots == 0 && a.g.begin[pair + 1] > a.g.begin[pair]) return;   // written already
-  const int64_t quads = static_cast<int64_t>(a.rank) * a.C / 4;
+// Both gradients in one launch: the first blocks_a blocks dA's, the others dB's.
+template <int DT, int MR>
+__global__ __launch_bounds__(kGradThreads) void gradient_kernel(BothGrads b) {
+  constexpr int P = DT == MOE_F16 ? 2 : 3;
+  __shared__ __attribute__((aligned(16))) unsigned char z_lds[kGradRows * kGradColumns * 2];
+  __shared__ __attribute__((aligned(16))) unsigned char u_lds[P * 16 * MR * kLowStride];
+  __shared__ float wave_top[4];
+  if (static_cast<int>(blockIdx.x) < b.blocks_a) gradient_piece<DT, MR, false>(b, b.of[0], blockIdx.x, z_lds, u_lds, wave_top);
+  else gradient_piece<DT, MR, true>(b, b.of[1], blockIdx.x - b.blocks_a, z_lds, u_lds, wave_top);
+}
+
+// Pairs without rows: zeros; of several pieces: the partial sums in order.  per_pair[t] blocks per pair for gradient t.
+struct FinishArgs {
+  BothGrads b;
+  int per_pair[2];
+  bool no_rows;     // nothing was counted: zeros everywhere
+};
+__global__ __launch_bounds__(256) void finish_kernel(FinishArgs f) {
+  const int t = static_cast<int>(blockIdx.x) < f.b.pairs * f.per_pair[0] ? 0 : 1;
+  const GradArgs& a = f.b.of[t];
+  const int block = blockIdx.x - t * f.b.pairs * f.per_pair[0];
+  const int pair = block / f.per_pair[t], part = block - pair * f.per_pair[t];
+  int slot = 0, slots = 0;
+  if (!f.no_rows) {
+    slot = a.pieces.slot[pair];
+    slots = a.pieces.slot[pair + 1] - slot;
+    if (slots == 0 && f.b.g.begin[pair + 1] > f.b.g.begin[pair]) return;   // written already
+  }
+  const int64_t quads = static_cast<int64_t>(f.b.rank) * a.C / 4;
   f32x4* out = reinterpret_cast<f32x4*>(a.out) + pair * quads;
   const f32x4* in = reinterpret_cast<const f32x4*>(a.partial) + slot * quads;
-  for (int64_t q = static_cast<int64_t>(part) * 256 + threadIdx.x; q < quads; q += static_cast<int64_t>(per_pair) * 256) {
+  for (int64_t q = static_cast<int64_t>(part) * 256 + threadIdx.x; q < quads; q += static_cast<int64_t>(f.per_pair[t]) * 256) {
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < slots; ++k) v += in[k * quads + q];
+    for (int k = 0; k < slots; k += 4) {
+      f32x4 p[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = in[min(k + i, slots - 1) * quads + q];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (k + i < slots) v += p[i];
+    }
     out[q] = v;
   }
 }
@@ -448,21 +564,38 @@ int check_config(const moe_adapter_config* c) {
   return MOE_OK;
 }
 
-// Rows of a piece of the gradients: at least 256, so that a launch has some 32 pieces at most per pair that has all the rows.
-int rows_of_piece(const moe_adapter_config& c) {
-  const int64_t n = ((static_cast<int64_t>(c.rows) + 31) / 32 + kGradRows - 1) / kGradRows * kGradRows;
-  return static_cast<int>(n < 256 ? 256 : n);
+// Rows of a piece of a gradient of C columns: so many pieces that there are some 512 blocks, two per CU, if one pair has all the
+// rows; 128 at least (fewer would write and read more partial sums than they read of z: rank * C floats per piece).
+int rows_of_piece(const moe_adapter_config& c, int C) {
+  const int64_t col_blocks = (C + kGradColumns - 1) / kGradColumns;
+  const int64_t n = (c.rows * col_blocks + 511) / 512;
+  return static_cast<int>(n < 128 ? 128 : (n + kGradRows - 1) / kGradRows * kGradRows);
 }
-int64_t most_pieces(const moe_adapter_config& c) {
+int64_t most_pieces(const moe_adapter_config& c, int C) {
   const int64_t pairs = static_cast<int64_t>(c.n_exp) * c.n_adapters;
-  return c.rows / rows_of_piece(c) + 1 + (pairs < c.rows ? pairs : c.rows);
+  return c.rows / rows_of_piece(c, C) + 1 + (pairs < c.rows ? pairs : c.rows);
 }
 // A pair of several pieces has more rows than one piece: at most two slots per full piece.
-int64_t most_slots(const moe_adapter_config& c) { return 2 * (static_cast<int64_t>(c.rows) / rows_of_piece(c)) + 1; }
+int64_t most_slots(const moe_adapter_config& c, int C) { return 2 * (static_cast<int64_t>(c.rows) / rows_of_piece(c, C)) + 1; }
+
+// Rows of a block and cuts of the contraction: 32 rows (64 at ranks above 32), or fewer while that leaves CUs without a block (a
+// row's own adapter is a block's whole work then), down to 16 where the matrices weigh more than the rows and the contraction can be cut.
+void shape_of_shrink(int64_t rows, int rank, int K, int* tile_rows, int* cuts) {
+  int t = rank > 32 ? 64 : 32;
+  const int least = rank > 32 && rows > 512 ? 16 : 1;
+  *cuts = 1;
+  while (t > 16 && (rows + t / 2 - 1) / (t / 2) <= 256 && !(rank > 32 && rows > 512)) t /= 2;
+  while (t <= 16 && t > least && (rows + t / 2 - 1) / (t / 2) <= 256) t /= 2;
+  if (rank > 32 && rows > 512) {
+    const int64_t tiles = (rows + t - 1) / t;
+    while (*cuts < 8 && tiles * *cuts * 2 <= 256 && K / (*cuts * 2) >= 1024) *cuts *= 2;
+  }
+  *tile_rows = t;
+}
 
 struct Layout {
-  size_t of_row, low, gemm, total;                                                        // forward and backward
-  size_t t, At, Bt, begin, piece_begin, slot_begin, piece_pair, list, partial_a, partial_b;   // backward
+  size_t of_row, low, gemm, cut, total;                                                   // forward and backward
+  size_t t, At, Bt, begin, list, ticket, piece_begin[2], slot[2], piece_pair[2], partial[2];   // backward
 };
 
 Layout layout_of(const moe_adapter_config& c, bool backward) {
@@ -477,17 +610,23 @@ Layout layout_of(const moe_adapter_config& c, bool backward) {
   L.of_row = take(rows * 4);
   L.low = take(rows * c.rank * 2);
   L.gemm = take(grouped_gemm_workspace_bytes());
+  int tile_rows = 0, cuts = 1;
+  shape_of_shrink(c.rows, c.rank, backward ? c.N : c.K, &tile_rows, &cuts);
+  L.cut = take(cuts > 1 ? cuts * rows * c.rank * 4 : 0);
   if (backward) {
     L.t = take(rows * c.rank * 4);
     L.At = take(pairs * c.rank * c.K * 2);
     L.Bt = take(pairs * c.rank * c.N * 2);
     L.begin = take((pairs + 1) * 4);
-    L.piece_begin = take((pairs + 1) * 4);
-    L.slot_begin = take((pairs + 1) * 4);
-    L.piece_pair = take(most_pieces(c) * 4);
     L.list = take(rows * 4);
-    L.partial_a = take(most_slots(c) * c.rank * c.K * 4);
-    L.partial_b = take(most_slots(c) * c.rank * c.N * 4);
+    L.ticket = take(4);
+    for (int t = 0; t < 2; ++t) {
+      const int C = t == 0 ? c.K : c.N;
+      L.piece_begin[t] = take((pairs + 1) * 4);
+      L.slot[t] = take((pairs + 1) * 4);
+      L.piece_pair[t] = take(most_pieces(c, C) * 4);
+      L.partial[t] = take(most_slots(c, C) * c.rank * C * 4);
+    }
   }
   L.total = off;
   return L;
@@ -495,17 +634,43 @@ Layout layout_of(const moe_adapter_config& c, bool backward) {
 
 template <int DT>
 hipError_t launch_shrink_of(const ShrinkArgs& a, int64_t rows, hipStream_t s) {
-  const unsigned grid = static_cast<unsigned>((rows + a.tile_rows - 1) / a.tile_rows);
-  if (a.rank <= 16) shrink_kernel<DT, 1, 8><<<grid, 512, 0, s>>>(a);
-  else if (a.rank <= 32) shrink_kernel<DT, 2, 8><<<grid, 512, 0, s>>>(a);
-  else if (a.rank <= 64) shrink_kernel<DT, 4, 8><<<grid, 512, 0, s>>>(a);
-  else shrink_kernel<DT, 8, 4><<<grid, 256, 0, s>>>(a);   // (the partial sums' place in LDS)
+  const int64_t tiles = (rows + a.tile_rows - 1) / a.tile_rows * a.cuts;
+  const unsigned grid = static_cast<unsigned>((tiles + 7) / 8 * 8);   // (every XCD the same run of tiles)
+#define PPMOE_SHRINK(MR, WAVES, G, J)                                                                      \
+  do {                                                                                                     \
+    constexpr int kLds = sizeof(float) * WAVES * 16 * G * (16 * MR + 4);                                   \
+    if (kLds > 65536) {                                                                                    \
+      static std::atomic<uint64_t> done{0};                                                                \
+      const hipError_t e = once_per_device(done, [] {                                                      \
+        return hipFuncSetAttribute(reinterpret_cast<const void*>(shrink_kernel<DT, MR, WAVES, G, J>),      \
+                                   hipFuncAttributeMaxDynamicSharedMemorySize, kLds);                      \
+      });                                                                                                  \
+      if (e != hipSuccess) return e;                                                                       \
+    }                                                                                                      \
+    shrink_kernel<DT, MR, WAVES, G, J><<<grid, 64 * WAVES, kLds, s>>>(a);                                  \
+  } while (0)
+  if (a.tile_rows > 32) {
+    if (a.rank <= 64) PPMOE_SHRINK(4, 8, 4, 2);
+    else PPMOE_SHRINK(8, 4, 4, 1);
+  } else if (a.tile_rows > 16) {
+    if (a.rank <= 16) PPMOE_SHRINK(1, 8, 2, 4);
+    else if (a.rank <= 32) PPMOE_SHRINK(2, 8, 2, 4);
+    else if (a.rank <= 64) PPMOE_SHRINK(4, 8, 2, 2);
+    else PPMOE_SHRINK(8, 8, 2, 2);
+  } else if (a.rank <= 16) PPMOE_SHRINK(1, 8, 1, 8);
+  else if (a.rank <= 32) PPMOE_SHRINK(2, 8, 1, 4);
+  else if (a.rank <= 64) PPMOE_SHRINK(4, 8, 1, 4);
+  else PPMOE_SHRINK(8, 8, 1, 2);
+#undef PPMOE_SHRINK
+  if (a.cuts > 1) {
+    const int64_t blocks = (rows * (a.rank / 4) + 255) / 256;
+    combine_kernel<DT><<<static_cast<unsigned>(blocks < 4096 ? blocks : 4096), 256, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
-// Blocks of 16 rows, or of fewer while that leaves CUs without one (a row's own adapter is a block's whole work then).
 hipError_t launch_shrink(int dtype, ShrinkArgs a, int64_t rows, hipStream_t s) {
-  a.tile_rows = 16;
-  while (a.tile_rows > 1 && (rows + a.tile_rows / 2 - 1) / (a.tile_rows / 2) <= 256) a.tile_rows /= 2;
+  shape_of_shrink(rows, a.rank, a.K, &a.tile_rows, &a.cuts);
+  a.rows = static_cast<int>(rows);
   return dtype == MOE_F16 ? launch_shrink_of<MOE_F16>(a, rows, s) : launch_shrink_of<MOE_BF16>(a, rows, s);
 }
 
@@ -515,13 +680,13 @@ hipError_t launch_transpose(const void* in, void* out, int64_t batch, int R, int
   return hipGetLastError();
 }
 
-template <int DT, bool BY_COLUMN>
-hipError_t launch_gradient_of(const GradArgs& a, int64_t pieces, int64_t pairs, hipStream_t s) {
-  const unsigned grid = static_cast<unsigned>(pieces * ((a.C + kGradColumns - 1) / kGradColumns));
-  if (a.rank <= 16) gradient_kernel<DT, 1, BY_COLUMN><<<grid, kGradThreads, 0, s>>>(a);
-  else if (a.rank <= 32) gradient_kernel<DT, 2, BY_COLUMN><<<grid, kGradThreads, 0, s>>>(a);
-  else if (a.rank <= 64) gradient_kernel<DT, 4, BY_COLUMN><<<grid, kGradThreads, 0, s>>>(a);
-  else gradient_kernel<DT, 8, BY_COLUMN><<<grid, kGradThreads, 0, s>>>(a);
+template <int DT>
+hipError_t launch_gradients_of(const BothGrads& b, int64_t blocks, hipStream_t s) {
+  const unsigned grid = static_cast<unsigned>(blocks);
+  if (b.rank <= 16) gradient_kernel<DT, 1><<<grid, kGradThreads, 0, s>>>(b);
+  else if (b.rank <= 32) gradient_kernel<DT, 2><<<grid, kGradThreads, 0, s>>>(b);
+  else if (b.rank <= 64) gradient_kernel<DT, 4><<<grid, kGradThreads, 0, s>>>(b);
+  else gradient_kernel<DT, 8><<<grid, kGradThreads, 0, s>>>(b);
   return hipGetLastError();
 }
 
@@ -560,7 +725,7 @@ int moe_adapter_forward(const moe_adapter_config* cfg, const void* x, const int3
   int32_t* of_row = reinterpret_cast<int32_t*>(ws + L.of_row);
   bf16_t* low = reinterpret_cast<bf16_t*>(ws + L.low);
   adapter::ShrinkArgs a = {static_cast<const bf16_t*>(x), static_cast<const bf16_t*>(A), offsets, adapter, perm, scale, of_row, v, low,
-                           cfg->n_exp, cfg->n_adapters, cfg->top_k, cfg->K, cfg->rank, 0, false};
+                           cfg->n_exp, cfg->n_adapters, cfg->top_k, cfg->K, cfg->rank, 0, false, nullptr, reinterpret_cast<float*>(ws + L.cut), 1, 0};
   hipError_t e = adapter::launch_shrink(cfg->dtype, a, cfg->rows, s);
   if (e != hipSuccess) return MOE_ERR_HIP;
   const AdapterRows rows = {of_row, low, static_cast<const bf16_t*>(B), cfg->n_exp, cfg->rank};
@@ -598,7 +763,7 @@ int moe_adapter_backward(const moe_adapter_config* cfg, const void* x, const int
     e = adapter::launch_transpose(B, Bt, pairs, N, rank, s);
     if (e != hipSuccess) return MOE_ERR_HIP;
     adapter::ShrinkArgs a = {static_cast<const bf16_t*>(dy), Bt, offsets, adapter, perm, scale, of_row, t, low,
-                             n_exp, cfg->n_adapters, cfg->top_k, N, rank, 0, true};
+                             n_exp, cfg->n_adapters, cfg->top_k, N, rank, 0, true, reinterpret_cast<int32_t*>(ws + L.ticket), reinterpret_cast<float*>(ws + L.cut), 1, 0};
     e = adapter::launch_shrink(cfg->dtype, a, cfg->rows, s);
     if (e != hipSuccess) return MOE_ERR_HIP;
     if (dx != nullptr) {
@@ -610,34 +775,36 @@ int moe_adapter_backward(const moe_adapter_config* cfg, const void* x, const int
       if (e != hipSuccess) return MOE_ERR_HIP;
     }
   }
-  adapter::Groups g = {reinterpret_cast<int32_t*>(ws + L.begin), reinterpret_cast<int32_t*>(ws + L.piece_begin),
-                       reinterpret_cast<int32_t*>(ws + L.slot_begin), reinterpret_cast<int32_t*>(ws + L.piece_pair),
-                       reinterpret_cast<int32_t*>(ws + L.list)};
-  const int most = adapter::rows_of_piece(*cfg);
+  auto words = [&](size_t off) { return reinterpret_cast<int32_t*>(ws + off); };
+  adapter::FinishArgs f = {};
+  f.no_rows = cfg->rows == 0;
+  adapter::BothGrads& b = f.b;
+  b.g.begin = words(L.begin);
+  b.g.list = words(L.list);
+  b.g.ticket = words(L.ticket);
+  b.pairs = static_cast<int>(pairs);
+  b.n_exp = n_exp;
+  b.rank = rank;
+  int64_t blocks[2];
+  for (int i = 0; i < 2; ++i) {
+    const int C = i == 0 ? K : N;
+    b.g.pieces[i] = {words(L.piece_begin[i]), words(L.slot[i]), words(L.piece_pair[i]), adapter::rows_of_piece(*cfg, C)};
+    b.of[i] = {i == 0 ? t : v, i == 0 ? nullptr : scale, static_cast<const bf16_t*>(i == 0 ? x : dy), i == 0 ? dA : dB,
+               reinterpret_cast<float*>(ws + L.partial[i]), b.g.pieces[i], C};
+    blocks[i] = adapter::most_pieces(*cfg, C) * ((C + adapter::kGradColumns - 1) / adapter::kGradColumns);
+    const int64_t quads = static_cast<int64_t>(rank) * C / 4;
+    f.per_pair[i] = static_cast<int>(quads < 2048 ? 1 : quads / 1024 < 128 ? quads / 1024 : 128);
+  }
   const unsigned n_pairs = static_cast<unsigned>(pairs);
-  adapter::count_kernel<<<n_pairs, 256, 0, s>>>(of_row, offsets, n_exp, g.begin);
-  adapter::scan_kernel<<<1, 1024, 0, s>>>(g, static_cast<int>(pairs), most);
-  adapter::fill_kernel<<<n_pairs, 256, 0, s>>>(of_row, offsets, n_exp, g);
-  adapter::GradArgs ga = {t, nullptr, static_cast<const bf16_t*>(x), dA, reinterpret_cast<float*>(ws + L.partial_a), g,
-                          static_cast<int>(pairs), n_exp, rank, K, most};
-  adapter::GradArgs gb = {v, scale, static_cast<const bf16_t*>(dy), dB, reinterpret_cast<float*>(ws + L.partial_b), g,
-                          static_cast<int>(pairs), n_exp, rank, N, most};
   if (cfg->rows > 0) {
-    const int64_t pieces = adapter::most_pieces(*cfg);
-    if (cfg->dtype == MOE_F16) {
-      e = adapter::launch_gradient_of<MOE_F16, false>(ga, pieces, pairs, s);
-      if (e == hipSuccess) e = adapter::launch_gradient_of<MOE_F16, true>(gb, pieces, pairs, s);
-    } else {
-      e = adapter::launch_gradient_of<MOE_BF16, false>(ga, pieces, pairs, s);
-      if (e == hipSuccess) e = adapter::launch_gradient_of<MOE_BF16, true>(gb, pieces, pairs, s);
-    }
+    b.blocks_a = static_cast<int>(blocks[0]);
+    adapter::count_kernel<<<n_pairs, 256, 0, s>>>(of_row, offsets, n_exp, b.g, b.pairs);
+    adapter::fill_kernel<<<n_pairs, 256, 0, s>>>(of_row, offsets, n_exp, b.g);
+    e = cfg->dtype == MOE_F16 ? adapter::launch_gradients_of<MOE_F16>(b, blocks[0] + blocks[1], s)
+                              : adapter::launch_gradients_of<MOE_BF16>(b, blocks[0] + blocks[1], s);
     if (e != hipSuccess) return MOE_ERR_HIP;
   }
-  for (const adapter::GradArgs& q : {ga, gb}) {
-    const int64_t quads = static_cast<int64_t>(rank) * q.C / 4;
-    const int per_pair = static_cast<int>(quads < 1024 ? 1 : quads / 1024 < 64 ? quads / 1024 : 64);
-    adapter::finish_kernel<<<n_pairs * per_pair, 256, 0, s>>>(q, per_pair);
-  }
+  adapter::finish_kernel<<<n_pairs * (f.per_pair[0] + f.per_pair[1]), 256, 0, s>>>(f);
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 

@@ -4,15 +4,17 @@
 //
 // low [rows, rank] 16-bit (scaled already), up [n_adapters, n_exp, Nout, rank] 16-bit.  rank is a multiple of 8, so an adapter is
 // rank / 8 pieces of 16 bytes per row of either matrix: what a lane holds of a matrix instruction's operand.  A
-// wavefront goes through the adapters that its rows have, in ascending order, and packs their pieces into k-steps one behind the
-// other (two adapters of rank 16 share a step of 32): a row's operand is zero at other adapters' pieces.  Both operands
-// come straight from memory: it is a step or two per tile where the rows are whole requests, next to the 32 of a contraction of 1024.
+// wavefront goes through the adapters that its rows have, in ascending order; a row's operand is zero where it has another
+// one.  Both operands come straight from memory: it is a step or two per tile where the rows are whole requests, next to the 32 of a
+// contraction of 1024.
 //
 // 0 * infinity would carry an adapter's infinities and NaNs to other requests' rows.  They are looked for in the operand,
-// replaced by zeros where there are any, and the blocks of R columns they are in become NaN in that adapter's own rows.
+// replaced by zeros where there are any, and the blocks of columns they are in become NaN in that adapter's own rows.
 #pragma once
 
-#include "common.h"
+#include <type_traits>
+
+#include "gemm_core.h"
 
 namespace ppmoe {
 
@@ -23,27 +25,29 @@ struct NonFinite {   // marks (in bits 15 and 31) the elements of a word whose e
   static __device__ __forceinline__ uint32_t cleared(uint32_t w) { return w & ~((marks(w) >> 15) * 0xffffu); }
 };
 
-// Names accumulators as accumulator registers at this point of the program (R = 16: the persistent kernel's 256; left to
-// itself the register allocator moves some of them to vector registers and spills).
-template <int MI, int NI, typename ACC>
-__device__ __forceinline__ void hold(ACC& acc) {
+constexpr int kNone = 0x7fffffff;   // after the last adapter
+
+// The least adapter above a among this lane's rows and those of the 15 lanes beside it.
+template <int MI>
+__device__ __forceinline__ int least_above(const int (&mine)[MI], int a) {
+  int least = kNone;
 #pragma unroll
-  for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-    for (int ni = 0; ni < NI; ++ni) asm volatile("" : "+a"(acc[mi][ni]));
+  for (int mi = 0; mi < MI; ++mi) least = mine[mi] > a && mine[mi] < least ? mine[mi] : least;
+  least = min(least, __builtin_amdgcn_update_dpp(0, least, 0x128, 0xf, 0xf, true));   // row_ror:8, 4, 2, 1
+  least = min(least, __builtin_amdgcn_update_dpp(0, least, 0x124, 0xf, 0xf, true));
+  least = min(least, __builtin_amdgcn_update_dpp(0, least, 0x122, 0xf, 0xf, true));
+  return min(least, __builtin_amdgcn_update_dpp(0, least, 0x121, 0xf, 0xf, true));
 }
 
-// R: 16 or 32, rows and columns of a matrix instruction (16x16x32, 32x32x16): a k-step has 64 / R pieces.  acc[mi][ni] += the block of
-// rows row0 + mi R .. and columns col0 + ni R .. of this wavefront; rows from `nrow` on are not looked at, columns past the
-// last one read the last one (neither is stored).  Accumulator layout: row lane % R, columns by register.
-template <int DT, int R, int MI, int NI, typename ACC>
-__device__ __forceinline__ void add_low_rank(ACC& acc, const AdapterRows& ad, int expert, int row0, int nrow, int col0, int Nout) {
+// The kernels of 32x32x16 instructions: a k-step has two pieces, which may be two adapters' (rank 8).  acc[mi][ni] += the block of
+// rows row0 + 32 mi .. and columns col0 + 32 ni .. of this wavefront; rows from `nrow` on are not looked at, columns past the
+// last one read the last one (neither is stored).  Accumulator layout: row lane % 32, columns by register.
+template <int DT, int MI, int NI>
+__device__ __forceinline__ void add_low_rank32(f32x16 (&acc)[MI][NI], const AdapterRows& ad, int expert, int row0, int nrow, int col0, int Nout) {
   typedef typename Elem16<DT>::vec8 vec8;
-  constexpr int kSlots = 64 / R;
-  constexpr int kNone = 0x7fffffff;
+  constexpr int R = 32, kSlots = 2;
   const u32x4 zero = u32x4{0u, 0u, 0u, 0u};
-  int lane = threadIdx.x & 63;
-  asm volatile("" : "+v"(lane));   // (what follows is computed here, not kept across the caller's K loop)
+  const int lane = threadIdx.x & 63;
   const int fr = lane & (R - 1), fq = lane / R;
   int mine[MI];
 #pragma unroll
@@ -51,13 +55,8 @@ __device__ __forceinline__ void add_low_rank(ACC& acc, const AdapterRows& ad, in
     const int r = mi * R + fr;
     mine[mi] = r < nrow ? ad.of_row[row0 + r] : -1;
   }
-  auto next_after = [&](int a) __attribute__((always_inline)) -> int {   // the least adapter above a among the rows
-    int least = kNone;
-#pragma unroll
-    for (int mi = 0; mi < MI; ++mi) least = mine[mi] > a && mine[mi] < least ? mine[mi] : least;
-#pragma unroll
-    for (int off = R / 2; off >= 1; off >>= 1) least = min(least, __shfl_xor(least, off, 64));
-    return __builtin_amdgcn_readfirstlane(least);
+  auto next_after = [&](int a) __attribute__((always_inline)) -> int {
+    return __builtin_amdgcn_readfirstlane(min(least_above(mine, a), __shfl_xor(least_above(mine, a), 16, 64)));
   };
   const int pieces = ad.rank >> 3;
   int at = next_after(-1), piece = 0;
@@ -110,12 +109,9 @@ __device__ __forceinline__ void add_low_rank(ACC& acc, const AdapterRows& ad, in
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni) {
         const vec8 u = __builtin_bit_cast(vec8, up[ni]), l = __builtin_bit_cast(vec8, low[mi]);
-        if constexpr (R == 16) acc[mi][ni] = Elem16<DT>::mfma16(u, l, acc[mi][ni]);
-        else acc[mi][ni] = Elem16<DT>::mfma32(u, l, acc[mi][ni]);
+        acc[mi][ni] = Elem16<DT>::mfma32(u, l, acc[mi][ni]);
       }
-    if constexpr (R == 16) hold<MI, NI>(acc);
     if (any) {
-      // (as products: accumulators that a branch changed element by element would all pass through vector registers)
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni) {
         if (bad[ni] == 0) continue;
@@ -125,12 +121,119 @@ __device__ __forceinline__ void add_low_rank(ACC& acc, const AdapterRows& ad, in
         for (int mi = 0; mi < MI; ++mi) {
           const uint32_t w = slot && my_a >= 0 && mine[mi] == my_a ? 0x7fff7fffu : 0u;
           const vec8 l = __builtin_bit_cast(vec8, u32x4{w, w, w, w});
-          if constexpr (R == 16) acc[mi][ni] = Elem16<DT>::mfma16(u, l, acc[mi][ni]);
-          else acc[mi][ni] = Elem16<DT>::mfma32(u, l, acc[mi][ni]);
+          acc[mi][ni] = Elem16<DT>::mfma32(u, l, acc[mi][ni]);
         }
-        if constexpr (R == 16) hold<MI, NI>(acc);
+          }
+    }
+  }
+}
+
+// Names accumulators as accumulator registers at this point of the program (left to itself the
+// register allocator moves some of them to vector registers and spills).
+template <int MI, int NI, typename ACC>
+__device__ __forceinline__ void hold(ACC& acc) {
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) asm volatile("" : "+a"(acc[mi][ni]));
+}
+
+// The persistent kernel's wavefront: 8 x NI blocks of 16x16x32 instructions, mine[mi] the adapter of row 16 mi + lane % 16 (-1: none,
+// or not a row of the tile), row0 and col0 its first row and column.  A step is up to 32 of one adapter's rank; blocks of 16
+// rows of which none has the adapter are passed over (8192 rows of 24 requests over 8 experts: four adapters per wavefront, each
+// in a third of its rows), so a step is little work and what it costs is the latency of its operands.
+template <int DT, int NI>
+__device__ __forceinline__ void add_low_rank16(f32x4 (&acc)[8][NI], const AdapterRows& ad, const int (&mine)[8], int expert, int row0,
+                                               int col0, int Nout) {
+  typedef typename Elem16<DT>::vec8 vec8;
+  constexpr int MI = 8;
+  int at = __builtin_amdgcn_readfirstlane(least_above(mine, -1)), piece0 = 0;
+  const int ncol = Nout - col0;
+  if (at == kNone || ncol <= 0) return;
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));   // (what follows is computed here, not kept across the K loop)
+  const int fr = lane & 15, fq = lane >> 4;
+  const int pieces = ad.rank >> 3, row_bytes = ad.rank * 2;
+  constexpr uint32_t kOutside = 0x80000000u;   // no descriptor covers it: the lane gets zeros
+  const __amdgpu_buffer_rsrc_t low_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<bf16_t*>(ad.low + static_cast<int64_t>(row0) * ad.rank), 0, 0x7fffffff, 0x00020000);
+  // Half of the columns at a time: while one half's operand is multiplied the other half's, or the next step's, is on its
+  // way, and a row block's takes the next step's place as soon as both halves have used it (64 registers; more of them in flight
+  // spill, and cost more than they hide).
+  constexpr int H = NI / 2;
+  u32x4 up[2][H], low[MI];
+  auto fetch_up = [&](u32x4 (&u)[H], int first) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<bf16_t*>(ad.up + ((static_cast<int64_t>(at) * ad.n_exp + expert) * Nout + col0) * ad.rank), 0, 0x7fffffff, 0x00020000);
+#pragma unroll
+    for (int ni = 0; ni < H; ++ni) {
+      const uint32_t off = min((first + ni) * 16 + fr, ncol - 1) * row_bytes + fq * 16;
+      u[ni] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, piece0 + fq < pieces ? off : kOutside, piece0 * 16, 0);
+    }
+  };
+  auto fetch_low = [&](int mi) __attribute__((always_inline)) {
+    const bool is = mine[mi] == at;
+    if (__ballot(is) != 0)
+      low[mi] = __builtin_amdgcn_raw_buffer_load_b128(low_rsrc, is && piece0 + fq < pieces ? (mi * 16 + fr) * row_bytes + fq * 16 : kOutside,
+                                                      piece0 * 16, 0);
+  };
+  auto clean = [&](u32x4 (&u)[H], auto first_c, int now) __attribute__((always_inline)) {
+    constexpr int first = decltype(first_c)::value;
+    uint32_t marks = 0;
+#pragma unroll
+    for (int ni = 0; ni < H; ++ni)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) marks |= NonFinite<DT>::marks(u[ni][q]);
+    if (__ballot(marks != 0) == 0) return;
+#pragma unroll
+    for (int ni = 0; ni < H; ++ni) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        m |= NonFinite<DT>::marks(u[ni][q]);
+        u[ni][q] = NonFinite<DT>::cleared(u[ni][q]);
+      }
+      if (__ballot(m != 0) != 0) {
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+          const uint32_t w = mine[mi] == now ? 0x7fff7fffu : 0u;
+          acc[mi][first + ni] = Elem16<DT>::mfma16(__builtin_bit_cast(vec8, u[ni]), __builtin_bit_cast(vec8, u32x4{w, w, w, w}), acc[mi][first + ni]);
+        }
       }
     }
+    hold<MI, NI>(acc);
+  };
+  auto multiply = [&](u32x4 (&u)[H], auto first_c, int now, bool more) __attribute__((always_inline)) {
+    constexpr int first = decltype(first_c)::value;
+    clean(u, first_c, now);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      if (__ballot(mine[mi] == now) != 0) {
+#pragma unroll
+        for (int ni = 0; ni < H; ++ni)
+          acc[mi][first + ni] = Elem16<DT>::mfma16(__builtin_bit_cast(vec8, u[ni]), __builtin_bit_cast(vec8, low[mi]), acc[mi][first + ni]);
+      }
+      if (first > 0 && more) fetch_low(mi);
+    }
+    hold<MI, NI>(acc);
+  };
+  fetch_up(up[0], 0);
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi) fetch_low(mi);
+#pragma clang loop unroll(disable)
+  while (true) {
+    fetch_up(up[1], H);
+    const int now = at;
+    multiply(up[0], std::integral_constant<int, 0>{}, now, false);
+    piece0 += 4;
+    if (piece0 >= pieces) {
+      piece0 = 0;
+      at = __builtin_amdgcn_readfirstlane(least_above(mine, at));
+    }
+    const bool more = at != kNone;
+    if (more) fetch_up(up[0], 0);
+    multiply(up[1], std::integral_constant<int, H>{}, now, more);
+    if (!more) break;
   }
 }
 

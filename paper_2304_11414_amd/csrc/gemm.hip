@@ -190,7 +190,7 @@ __global__ __launch_bounds__(kGemmThreads) void grouped_gemm_bf16_kernel(
   }
 
   if constexpr (ADAPT)
-    add_low_rank<DT, 32, 4, 2>(acc, adapters, tc.expert, tc.row0 + wm * 128, tc.rows - wm * 128, tc.col0 + wn * 64, Nout);
+    add_low_rank32<DT, 4, 2>(acc, adapters, tc.expert, tc.row0 + wm * 128, tc.rows - wm * 128, tc.col0 + wn * 64, Nout);
 
   // ---- epilogue ------------------------------------------------------------------------------
   // D = W_frag (32 n) x Tok_frag^T (32 m): lane holds token column m = lane % 32 and, in register

@@ -301,7 +301,7 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_bwd_kernel(
   accumulate_tile<MODE, DT>(ti, acc, lds);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if constexpr (ADAPT)
-    add_low_rank<DT, 32, 2, 2>(acc, adapters, ti.expert, ti.row0 + (wave >> 1) * 64, ti.rows - (wave >> 1) * 64,
+    add_low_rank32<DT, 2, 2>(acc, adapters, ti.expert, ti.row0 + (wave >> 1) * 64, ti.rows - (wave >> 1) * 64,
                                ti.col0 + (wave & 1) * 64, N);
   store_tile_output<MODE, DT>(acc, C, ti, N, M, wave >> 1, wave & 1, lane & 31, lane >> 5);
 }
