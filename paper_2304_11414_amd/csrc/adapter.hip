@@ -194,19 +194,24 @@ __global__ __launch_bounds__(256) void combine_kernel(ShrinkArgs a) {
   }
 }
 
-// ---- [batch, R, C] -> [batch, C, R], 16-bit, both multiples of 8 ----------------------------------------
-__global__ __launch_bounds__(256) void transpose_kernel(const bf16_t* __restrict__ in, bf16_t* __restrict__ out, int R, int C,
-                                                        int r_tiles, int c_tiles) {
+// ---- [batch, R, C] -> [batch, C, R], 16-bit, both multiples of 8; two such tensors in one launch ---------------------
+struct Transpose {
+  const bf16_t* in;
+  bf16_t* out;
+  int R, C, r_tiles, c_tiles;   // tiles of 64 x 64
+};
+__global__ __launch_bounds__(256) void transpose_kernel(Transpose t0, Transpose t1, unsigned blocks0) {
   __shared__ uint16_t tile[64][66];
-  const int64_t per = static_cast<int64_t>(r_tiles) * c_tiles, batch = blockIdx.x / per;
-  const int t = static_cast<int>(blockIdx.x - batch * per);
-  const int r0 = (t / c_tiles) * 64, c0 = (t % c_tiles) * 64;
-  const bf16_t* src = in + batch * R * C;
-  bf16_t* dst = out + batch * R * C;
+  const Transpose a = blockIdx.x < blocks0 ? t0 : t1;
+  const unsigned block = blockIdx.x < blocks0 ? blockIdx.x : blockIdx.x - blocks0;
+  const unsigned per = static_cast<unsigned>(a.r_tiles) * a.c_tiles, batch = block / per, t = block - batch * per;
+  const int r0 = static_cast<int>(t / a.c_tiles) * 64, c0 = static_cast<int>(t % a.c_tiles) * 64;
+  const bf16_t* src = a.in + static_cast<int64_t>(batch) * a.R * a.C;
+  bf16_t* dst = a.out + static_cast<int64_t>(batch) * a.R * a.C;
   for (int p = threadIdx.x; p < 64 * 8; p += 256) {
     const int r = p >> 3, c = (p & 7) * 8;
-    if (r0 + r < R && c0 + c < C) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(src + static_cast<int64_t>(r0 + r) * C + c0 + c);
+    if (r0 + r < a.R && c0 + c < a.C) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(src + static_cast<int64_t>(r0 + r) * a.C + c0 + c);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         tile[r][c + 2 * q] = static_cast<uint16_t>(v[q]);
@@ -217,11 +222,11 @@ __global__ __launch_bounds__(256) void transpose_kernel(const bf16_t* __restrict
   __syncthreads();
   for (int p = threadIdx.x; p < 64 * 8; p += 256) {
     const int c = p >> 3, r = (p & 7) * 8;
-    if (c0 + c < C && r0 + r < R) {
+    if (c0 + c < a.C && r0 + r < a.R) {
       u32x4 v;
 #pragma unroll
       for (int q = 0; q < 4; ++q) v[q] = tile[r + 2 * q][c] | (static_cast<uint32_t>(tile[r + 2 * q + 1][c]) << 16);
-      *reinterpret_cast<u32x4*>(dst + static_cast<int64_t>(c0 + c) * R + r0 + r) = v;
+      *reinterpret_cast<u32x4*>(dst + static_cast<int64_t>(c0 + c) * a.R + r0 + r) = v;
     }
   }
 }
@@ -674,11 +679,10 @@ hipError_t launch_shrink(int dtype, ShrinkArgs a, int64_t rows, hipStream_t s) {
   return dtype == MOE_F16 ? launch_shrink_of<MOE_F16>(a, rows, s) : launch_shrink_of<MOE_BF16>(a, rows, s);
 }
 
-hipError_t launch_transpose(const void* in, void* out, int64_t batch, int R, int C, hipStream_t s) {
-  const int rt = (R + 63) / 64, ct = (C + 63) / 64;
-  transpose_kernel<<<static_cast<unsigned>(batch * rt * ct), 256, 0, s>>>(static_cast<const bf16_t*>(in), static_cast<bf16_t*>(out), R, C, rt, ct);
-  return hipGetLastError();
+Transpose transpose_of(const void* in, void* out, int R, int C) {
+  return {static_cast<const bf16_t*>(in), static_cast<bf16_t*>(out), R, C, (R + 63) / 64, (C + 63) / 64};
 }
+unsigned blocks_of(const Transpose& t, int64_t batch) { return static_cast<unsigned>(batch * t.r_tiles * t.c_tiles); }
 
 template <int DT>
 hipError_t launch_gradients_of(const BothGrads& b, int64_t blocks, hipStream_t s) {
@@ -759,16 +763,15 @@ int moe_adapter_backward(const moe_adapter_config* cfg, const void* x, const int
   bf16_t *At = reinterpret_cast<bf16_t*>(ws + L.At), *Bt = reinterpret_cast<bf16_t*>(ws + L.Bt);
   hipError_t e = hipSuccess;
   if (cfg->rows > 0) {
-    // t, of the contraction over N that B has as its rows
-    e = adapter::launch_transpose(B, Bt, pairs, N, rank, s);
-    if (e != hipSuccess) return MOE_ERR_HIP;
+    // The contractions over what A and B have as their rows: t, and the low-rank part of dx.
+    const adapter::Transpose tb = adapter::transpose_of(B, Bt, N, rank), ta = adapter::transpose_of(A, At, rank, K);
+    const unsigned blocks_b = adapter::blocks_of(tb, pairs), blocks_a = dx != nullptr ? adapter::blocks_of(ta, pairs) : 0;
+    adapter::transpose_kernel<<<blocks_b + blocks_a, 256, 0, s>>>(tb, ta, blocks_b);
     adapter::ShrinkArgs a = {static_cast<const bf16_t*>(dy), Bt, offsets, adapter, perm, scale, of_row, t, low,
                              n_exp, cfg->n_adapters, cfg->top_k, N, rank, 0, true, reinterpret_cast<int32_t*>(ws + L.ticket), reinterpret_cast<float*>(ws + L.cut), 1, 0};
     e = adapter::launch_shrink(cfg->dtype, a, cfg->rows, s);
     if (e != hipSuccess) return MOE_ERR_HIP;
     if (dx != nullptr) {
-      e = adapter::launch_transpose(A, At, pairs, rank, K, s);
-      if (e != hipSuccess) return MOE_ERR_HIP;
       const AdapterRows rows = {of_row, low, At, n_exp, rank};
       e = launch_data_gradient(cfg->dtype, static_cast<const bf16_t*>(dy), static_cast<const bf16_t*>(W), static_cast<bf16_t*>(dx),
                                offsets, n_exp, cfg->rows, cfg->rows, K, N, ws + L.gemm, s, &rows);

@@ -614,7 +614,10 @@ hipError_t launch_data_gradient(int dtype, const bf16_t* a, const bf16_t* b, bf1
   if (e != hipSuccess) return e;
   const int n_cus = cus_of_current_device() & ~7;
   auto few = [&](int64_t r) { return 2 * ((r + 255) / 256 + n_exp) * ((n + 255) / 256) < n_cus; };
-  const bool big = k % BK == 0 && k < (1 << 22) && n < kColumnsByRows && !few(rows);
+  // (With adapters also few tiles of a long contraction, which that kernel cuts between CUs.  301 rows of 1024 from 4096: 62 us on
+  // the small tiles, 54 on the large; 130 of 8192 from 8192: 117 and 76; but 300 of 4096 from 1024: 24 and 36, and 64 of 2048 from 2048 31
+  // and 30.)
+  const bool big = k % BK == 0 && k < (1 << 22) && n < kColumnsByRows && (!few(rows) || (adapters != nullptr && k >= 4096));
   const int pick_cus = big && expected_rows < rows && few(expected_rows) ? n_cus : 0;
   if (big) {
     e = launch_grouped_gemm_fast(dtype, false, a, b, cc, offsets, n_exp, 0, n, k, gemm_ws, s, 0, nullptr, nullptr, 1, nullptr,
