@@ -379,7 +379,7 @@ struct BothGrads {
 
 template <int DT, int MR, bool BY_COLUMN>
 __device__ __forceinline__ void gradient_piece(const BothGrads& b, const GradArgs& a, int block, unsigned char* z_lds, unsigned char* u_lds,
-                                               float* wave_top) {
+                                               int (*ids)[kGradRows], float* wave_top) {
   typedef typename Elem16<DT>::vec8 vec8;
   constexpr int P = DT == MOE_F16 ? 2 : 3;   // summands
   const int col_blocks = (a.C + kGradColumns - 1) / kGradColumns;
@@ -415,6 +415,14 @@ __device__ __forceinline__ void gradient_piece(const BothGrads& b, const GradArg
     }
   }
 
+  // The rows' numbers are in LDS a stage ahead of their data: a load then waits for nothing.
+  auto number = [&](int k) __attribute__((always_inline)) -> int { return list[min(k, count - 1)]; };   // (threads of the first wavefront)
+  int upcoming = 0, now = 0;
+  if (tid < kGradRows) {
+    ids[0][tid] = number(tid);
+    upcoming = number(kGradRows + tid);
+  }
+  __syncthreads();
   // staging: z in 1024 pieces of 16 bytes, four per thread (row p / 16, piece p % 16); u in quads
   u32x4 zv[4];
   constexpr int kQuads = 16 * MR * kGradRows / 4 / kGradThreads;
@@ -423,12 +431,12 @@ __device__ __forceinline__ void gradient_piece(const BothGrads& b, const GradArg
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int p = tid + i * kGradThreads, row = k0 + (p >> 4), c = col0 + (p & 15) * 8;
-      zv[i] = row < count && c < a.C ? *reinterpret_cast<const u32x4*>(a.z + static_cast<int64_t>(list[row]) * a.C + c) : u32x4{0u, 0u, 0u, 0u};
+      zv[i] = row < count && c < a.C ? *reinterpret_cast<const u32x4*>(a.z + static_cast<int64_t>(ids[now][p >> 4]) * a.C + c) : u32x4{0u, 0u, 0u, 0u};
     }
 #pragma unroll
     for (int i = 0; i < kQuads; ++i) {
       const int p = tid + i * kGradThreads, q = p / (4 * MR), j = (p % (4 * MR)) * 4, row = k0 + q;
-      uv[i] = row < count && j < rank ? *reinterpret_cast<const f32x4*>(a.u + static_cast<int64_t>(list[row]) * rank + j) : f32x4{0.f, 0.f, 0.f, 0.f};
+      uv[i] = row < count && j < rank ? *reinterpret_cast<const f32x4*>(a.u + static_cast<int64_t>(ids[now][q]) * rank + j) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
   // 32-byte block b of row k at b ^ ((k & 3) + 4 ((k >> 3) & 1)): what 32 lanes of a transposing read touch falls on all banks
@@ -466,8 +474,13 @@ __device__ __forceinline__ void gradient_piece(const BothGrads& b, const GradArg
   for (int k0 = 0; k0 < count; k0 += kGradRows) {
     __syncthreads();
     store();
+    now ^= 1;
+    if (tid < kGradRows) ids[now][tid] = upcoming;
     __syncthreads();
-    if (k0 + kGradRows < count) load(k0 + kGradRows);
+    if (k0 + kGradRows < count) {
+      load(k0 + kGradRows);
+      if (tid < kGradRows) upcoming = number(k0 + 2 * kGradRows + tid);
+    }
     const int j = (lane >> 2) & 3;
 #pragma unroll
     for (int ks = 0; ks < kGradRows / 32; ++ks) {
@@ -516,8 +529,9 @@ __global__ __launch_bounds__(kGradThreads) void gradient_kernel(BothGrads b) {
   __shared__ __attribute__((aligned(16))) unsigned char z_lds[kGradRows * kGradColumns * 2];
   __shared__ __attribute__((aligned(16))) unsigned char u_lds[P * 16 * MR * kLowStride];
   __shared__ float wave_top[4];
-  if (static_cast<int>(blockIdx.x) < b.blocks_a) gradient_piece<DT, MR, false>(b, b.of[0], blockIdx.x, z_lds, u_lds, wave_top);
-  else gradient_piece<DT, MR, true>(b, b.of[1], blockIdx.x - b.blocks_a, z_lds, u_lds, wave_top);
+  __shared__ int ids[2][kGradRows];
+  if (static_cast<int>(blockIdx.x) < b.blocks_a) gradient_piece<DT, MR, false>(b, b.of[0], blockIdx.x, z_lds, u_lds, ids, wave_top);
+  else gradient_piece<DT, MR, true>(b, b.of[1], blockIdx.x - b.blocks_a, z_lds, u_lds, ids, wave_top);
 }
 
 // Pairs without rows: zeros; of several pieces: the partial sums in order.  per_pair[t] blocks per pair for gradient t.
