@@ -267,7 +267,14 @@ __global__ __launch_bounds__(256) void count_kernel(const int32_t* __restrict__ 
   {
     const int id = blockIdx.x / n_exp, expert = blockIdx.x - id * n_exp;
     int n = 0;
-    for (int r = offsets[expert] + threadIdx.x; r < offsets[expert + 1]; r += 256) n += of_row[r] == id;
+    const int end = offsets[expert + 1];
+    for (int r = offsets[expert] + threadIdx.x; r < end; r += 4 * 256) {   // (four loads under way)
+      int v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = of_row[min(r + i * 256, end - 1)];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) n += r + i * 256 < end && v[i] == id;
+    }
     n = sum_of_block(n, lds);
     if (threadIdx.x == 0) {
       __hip_atomic_store(g.begin + blockIdx.x, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -338,17 +345,29 @@ __global__ __launch_bounds__(256) void fill_kernel(const int32_t* __restrict__ o
     const int p0 = g.pieces[t].begin[pair], p1 = g.pieces[t].begin[pair + 1];
     for (int p = p0 + threadIdx.x; p < p1; p += 256) g.pieces[t].pair[p] = pair;
   }
+  // A thread has four neighbouring rows of 1024.
   const int end = offsets[expert + 1];
-  for (int r0 = offsets[expert]; r0 < end; r0 += 256) {
-    const int r = r0 + threadIdx.x;
-    const bool is = r < end && of_row[r] == id;
-    const uint64_t lanes = __ballot(is);
+  for (int r0 = offsets[expert]; r0 < end; r0 += 1024) {
+    const int r = r0 + threadIdx.x * 4;
+    int v[4], mine = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = of_row[min(r + i, end - 1)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mine += r + i < end && v[i] == id;
+    int before = mine;   // of the wavefront's lanes up to this one
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int o = __shfl_up(before, off, 64);
+      if (lane >= off) before += o;
+    }
     __syncthreads();
-    if (lane == 0) lds[wave] = __popcll(lanes);
+    if (lane == 63) lds[wave] = before;
     __syncthreads();
-    int base = at;
-    for (int w = 0; w < wave; ++w) base += lds[w];
-    if (is) g.list[base + __popcll(lanes & ((uint64_t(1) << lane) - 1))] = r;
+    int to = at + before - mine;
+    for (int w = 0; w < wave; ++w) to += lds[w];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (r + i < end && v[i] == id) g.list[to++] = r + i;
     at += lds[0] + lds[1] + lds[2] + lds[3];
   }
 }
@@ -356,12 +375,11 @@ __global__ __launch_bounds__(256) void fill_kernel(const int32_t* __restrict__ o
 // ---- G[pair][j, c] = sum over the pair's rows of s u[r, j] z[r, c] ------------------------------------------
 //
 // u [rows, rank] float32 (t, or v), z [rows, C] 16-bit (x, or dy).  dA is stored [rank, C], dB [C, rank] (BY_COLUMN).
-// A block takes one piece of a pair's rows and 128 columns, 64 rows at a time: z as it is into LDS and from there
-// across its rows into operands (transposing read), u as 16-bit summands, each the rounding of what those before it leave: three for
+// A block takes one piece of a pair's rows and 128 columns, 64 rows at a time: both as they are into LDS and from there
+// across their rows into operands (transposing read), u as 16-bit summands, each the rounding of what those before it leave: three for
 // bf16, two for fp16 (24 and 22 bits together), so that the result has float32's accuracy.  fp16: u is first brought
 // to a largest value of 2^13 by a power of two, exactly, as its small values have no 22 bits.
 constexpr int kGradColumns = 128, kGradThreads = 256, kGradRows = 64;
-constexpr int kLowStride = kGradRows * 2 + 16;   // bytes of a row of u's summands in LDS
 
 struct GradArgs {
   const float* u;
@@ -439,7 +457,11 @@ __device__ __forceinline__ void gradient_piece(const BothGrads& b, const GradArg
       uv[i] = row < count && j < rank ? *reinterpret_cast<const f32x4*>(a.u + static_cast<int64_t>(ids[now][q]) * rank + j) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
-  // 32-byte block b of row k at b ^ ((k & 3) + 4 ((k >> 3) & 1)): what 32 lanes of a transposing read touch falls on all banks
+  // 32-byte block b of row k of z at b ^ ((k & 3) + 4 ((k >> 3) & 1)): what 32 lanes of a transposing read touch falls on all banks; u's
+  // rows of 32 MR bytes the same way as far as they have blocks
+  auto u_swizzle = [](int k) __attribute__((always_inline)) -> int {
+    return (MR == 8 ? (k & 3) + 4 * ((k >> 3) & 1) : (k & 3) ^ ((k >> 3) & 1)) & (MR - 1);
+  };
   auto store = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -449,16 +471,20 @@ __device__ __forceinline__ void gradient_piece(const BothGrads& b, const GradArg
     }
 #pragma unroll
     for (int i = 0; i < kQuads; ++i) {
-      const int p = tid + i * kGradThreads, q = p / (4 * MR), j = (p % (4 * MR)) * 4;
+      const int p = tid + i * kGradThreads, q = p / (4 * MR), j = p % (4 * MR);
+      unsigned char* at = u_lds + q * (32 * MR) + ((j >> 2) ^ u_swizzle(q)) * 32 + (j & 3) * 8;
+      f32x4 rest = uv[i] * (s * up);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float rest = uv[i][e] * s * up;
+      for (int part = 0; part < P; ++part) {
+        const u32x2 o = {Elem16<DT>::pack2(rest[0], rest[1]), Elem16<DT>::pack2(rest[2], rest[3])};
+        *reinterpret_cast<u32x2*>(at + part * (kGradRows * 32 * MR)) = o;
+        float h[4];
+        Elem16<DT>::widen2(o[0], h[0], h[1]);
+        Elem16<DT>::widen2(o[1], h[2], h[3]);
 #pragma unroll
-        for (int part = 0; part < P; ++part) {
-          const uint16_t h = static_cast<uint16_t>(Elem16<DT>::pack2(rest, 0.f));
-          *reinterpret_cast<uint16_t*>(u_lds + part * (16 * MR * kLowStride) + (j + e) * kLowStride + q * 2) = h;
-          rest -= Elem16<DT>::widen(h);
-          if (!(fabsf(rest) < 3.0e38f)) rest = 0.f;   // (an infinity or a NaN is in the first summand whole)
+        for (int e = 0; e < 4; ++e) {
+          rest[e] -= h[e];
+          if (!(fabsf(rest[e]) < 3.0e38f)) rest[e] = 0.f;   // (an infinity or a NaN is in the first summand whole)
         }
       }
     }
@@ -469,7 +495,7 @@ __device__ __forceinline__ void gradient_piece(const BothGrads& b, const GradArg
   for (int mr = 0; mr < MR; ++mr)
 #pragma unroll
     for (int ni = 0; ni < 2; ++ni) acc[mr][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const uint32_t z0 = core::lds_address(z_lds);
+  const uint32_t z0 = core::lds_address(z_lds), u0 = core::lds_address(u_lds);
   load(0);
   for (int k0 = 0; k0 < count; k0 += kGradRows) {
     __syncthreads();
@@ -491,13 +517,22 @@ __device__ __forceinline__ void gradient_piece(const BothGrads& b, const GradArg
         asm volatile("ds_read_b64_tr_b16 %0, %2\n\tds_read_b64_tr_b16 %1, %2 offset:1024"
                      : "=&v"(zt[ni][0]), "=&v"(zt[ni][1]) : "v"(at) : "memory");
       }
+      u32x2 ut[P][MR][2];
+      core::each<P * MR>([&](auto i) __attribute__((always_inline)) {
+        constexpr int part = i.value / MR, mr = i.value % MR;
+        const uint32_t at = u0 + (ks * 32 + fq * 8 + j) * (32 * MR) + ((mr ^ u_swizzle(fq * 8 + j)) << 5) + (lane & 3) * 8;
+        core::lds_read_transposed<part * (kGradRows * 32 * MR)>(ut[part][mr][0], at);
+        core::lds_read_transposed<part * (kGradRows * 32 * MR) + 4 * 32 * MR>(ut[part][mr][1], at);
+      });
+      asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(zt[0][0]), "+v"(zt[0][1]), "+v"(zt[1][0]), "+v"(zt[1][1]) : : "memory");
       vec8 u[P][MR];
 #pragma unroll
       for (int part = 0; part < P; ++part)
 #pragma unroll
-        for (int mr = 0; mr < MR; ++mr)
-          u[part][mr] = *reinterpret_cast<const vec8*>(u_lds + part * (16 * MR * kLowStride) + (mr * 16 + fr) * kLowStride + ks * 64 + fq * 16);
-      asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(zt[0][0]), "+v"(zt[0][1]), "+v"(zt[1][0]), "+v"(zt[1][1]) : : "memory");
+        for (int mr = 0; mr < MR; ++mr) {
+          asm volatile("" : "+v"(ut[part][mr][0]), "+v"(ut[part][mr][1]) : : "memory");
+          u[part][mr] = __builtin_bit_cast(vec8, __builtin_shufflevector(ut[part][mr][0], ut[part][mr][1], 0, 1, 2, 3));
+        }
 #pragma unroll
       for (int ni = 0; ni < 2; ++ni) {
         const vec8 z = __builtin_bit_cast(vec8, __builtin_shufflevector(zt[ni][0], zt[ni][1], 0, 1, 2, 3));
@@ -527,7 +562,7 @@ template <int DT, int MR>
 __global__ __launch_bounds__(kGradThreads) void gradient_kernel(BothGrads b) {
   constexpr int P = DT == MOE_F16 ? 2 : 3;
   __shared__ __attribute__((aligned(16))) unsigned char z_lds[kGradRows * kGradColumns * 2];
-  __shared__ __attribute__((aligned(16))) unsigned char u_lds[P * 16 * MR * kLowStride];
+  __shared__ __attribute__((aligned(16))) unsigned char u_lds[P * kGradRows * 32 * MR];
   __shared__ float wave_top[4];
   __shared__ int ids[2][kGradRows];
   if (static_cast<int>(blockIdx.x) < b.blocks_a) gradient_piece<DT, MR, false>(b, b.of[0], blockIdx.x, z_lds, u_lds, ids, wave_top);
