@@ -39,6 +39,31 @@ __device__ __forceinline__ int least_above(const int (&mine)[MI], int a) {
   return min(least, __builtin_amdgcn_update_dpp(0, least, 0x121, 0xf, 0xf, true));
 }
 
+// The kernels of few rows: four columns from `col` on of packed row `row`, which has adapter a >= 0.
+template <int DT>
+__device__ __forceinline__ f32x4 low_rank_of_four(const AdapterRows& ad, int row, int a, int expert, int col, int Nout) {
+  const u32x4* low = reinterpret_cast<const u32x4*>(ad.low + static_cast<int64_t>(row) * ad.rank);
+  const u32x4* up = reinterpret_cast<const u32x4*>(ad.up + ((static_cast<int64_t>(a) * ad.n_exp + expert) * Nout + col) * ad.rank);
+  const int pieces = ad.rank >> 3;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma clang loop unroll(disable)
+  for (int p = 0; p < pieces; ++p) {
+    const u32x4 l = low[p];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x4 u = up[i * pieces + p];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float l0, l1, u0, u1;
+        Elem16<DT>::widen2(l[q], l0, l1);
+        Elem16<DT>::widen2(u[q], u0, u1);
+        sum[i] = fmaf(l1, u1, fmaf(l0, u0, sum[i]));
+      }
+    }
+  }
+  return sum;
+}
+
 // The kernels of 32x32x16 instructions: a k-step has two pieces, which may be two adapters' (rank 8).  acc[mi][ni] += the block of
 // rows row0 + 32 mi .. and columns col0 + 32 ni .. of this wavefront; rows from `nrow` on are not looked at, columns past the
 // last one read the last one (neither is stored).  Accumulator layout: row lane % 32, columns by register.

@@ -306,6 +306,125 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_bwd_kernel(
   store_tile_output<MODE, DT>(acc, C, ti, N, M, wave >> 1, wave & 1, lane & 31, lane >> 5);
 }
 
+// The data gradient on few rows, with the rows' adapters:  C[r, n] = sum_k A[r, k] * B[i][k, n] (+ adapter_core.h).
+//
+// One pass over the weights per 64 rows of an expert, bound by their stream.  A block owns 64 columns of one expert, 128 bytes of each of B's rows;
+// its eight wavefronts split the contraction, 64 of B's rows at a time each: those go through LDS of the wavefront's own (4 KiB a
+// step of 32) and from there across the rows into operands (transposing read), A's rows come straight from memory.  The partial sums meet
+// in LDS, 16 rows at a time, and are added in wavefront order.
+namespace few_by_rows {
+
+constexpr int kWaves = 8, kColumns = 64, kLd = kColumns + 4;
+
+template <int DT>
+__global__ __launch_bounds__(64 * kWaves) void data_gradient_few_rows_kernel(const bf16_t* __restrict__ A, const bf16_t* __restrict__ B,
+                                                                             bf16_t* __restrict__ C, const int32_t* __restrict__ offsets,
+                                                                             int Nout, int K, AdapterRows adapters) {
+  typedef typename Elem16<DT>::vec8 vec8;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves * 16 * kLd * 4];
+  float (*part)[16][kLd] = reinterpret_cast<float (*)[16][kLd]>(lds);   // (after the loop: the partial sums)
+  const int n_tiles = (Nout + kColumns - 1) / kColumns;
+  const int expert = blockIdx.x / n_tiles, col0 = (blockIdx.x - expert * n_tiles) * kColumns;
+  const int lo = offsets[expert], cnt = offsets[expert + 1] - lo;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, fq = lane >> 4;
+  const u32x4 zero = u32x4{0u, 0u, 0u, 0u};
+  const bf16_t* Be = B + static_cast<int64_t>(expert) * K * Nout + col0;
+  // 32-byte block b of row k at b ^ (k & 3) ^ ((k >> 3) & 1): what 32 lanes of a transposing read touch falls on all banks
+  auto block_at = [](int k, int b) __attribute__((always_inline)) -> int { return (b ^ (k & 3) ^ ((k >> 3) & 1)) << 5; };
+  unsigned char* mine = lds + wave * 4096;
+  const uint32_t mine_at = core::lds_address(mine);
+  const int wrow = lane >> 3, wpiece = lane & 7;
+  const bool in_columns = col0 + wpiece * 8 < Nout;
+
+  auto pass = [&](int t0, int rows, auto mt_c) __attribute__((always_inline)) {
+    constexpr int MT = decltype(mt_c)::value, J = MT == 4 ? 1 : 2, kStep = 32 * J;   // (J 2 with MT 4 needs more than 256 registers)
+    const bf16_t* arow[MT];
+    f32x4 acc[MT][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      arow[mt] = A + static_cast<int64_t>(lo + t0 + min(mt * 16 + fr, rows - 1)) * K + fq * 8;   // (rows past the end re-read the last one)
+#pragma unroll
+      for (int nt = 0; nt < 4; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    u32x4 w[J][4], x[J][MT];
+    auto load = [&](int k0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int k = k0 + j * 32 + i * 8 + wrow;
+          w[j][i] = in_columns && k < K ? *reinterpret_cast<const u32x4*>(Be + static_cast<int64_t>(k) * Nout + wpiece * 8) : zero;
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          x[j][mt] = k0 + j * 32 + fq * 8 < K ? *reinterpret_cast<const u32x4*>(arow[mt] + k0 + j * 32) : zero;
+      }
+    };
+    load(wave * kStep);
+    for (int k0 = wave * kStep; k0 < K; k0 += kWaves * kStep) {
+      u32x4 a[J][MT];
+      u32x2 b[J][4][2];
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int k = i * 8 + wrow;
+          *reinterpret_cast<u32x4*>(mine + k * 128 + block_at(k, wpiece >> 1) + (wpiece & 1) * 16) = w[j][i];
+        }
+        const int q = (lane >> 2) & 3, kr = fq * 8 + q;
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt) {
+          const uint32_t at = mine_at + kr * 128 + block_at(kr, nt) + (lane & 3) * 8;
+          core::lds_read_transposed<0>(b[j][nt][0], at);
+          core::lds_read_transposed<512>(b[j][nt][1], at);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) a[j][mt] = x[j][mt];
+      }
+      if (k0 + kWaves * kStep < K) load(k0 + kWaves * kStep);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt) {
+          asm volatile("" : "+v"(b[j][nt][0]), "+v"(b[j][nt][1]) : : "memory");
+          const u32x4 f = __builtin_shufflevector(b[j][nt][0], b[j][nt][1], 0, 1, 2, 3);
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+            acc[mt][nt] = Elem16<DT>::mfma16(__builtin_bit_cast(vec8, f), __builtin_bit_cast(vec8, a[j][mt]), acc[mt][nt]);
+        }
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      __syncthreads();   // LDS has been read by every wavefront: its steps, or the partial sums before these
+      // D: lane: row fr, columns 4 fq + v
+#pragma unroll
+      for (int nt = 0; nt < 4; ++nt) *reinterpret_cast<f32x4*>(&part[wave][fr][nt * 16 + fq * 4]) = acc[mt][nt];
+      __syncthreads();
+      const int m = threadIdx.x >> 4, n = (threadIdx.x & 15) * 4;   // four columns of one row per thread
+      if (m < min(16, rows - mt * 16) && col0 + n < Nout) {
+        f32x4 v = *reinterpret_cast<const f32x4*>(&part[0][m][n]);
+#pragma unroll
+        for (int q = 1; q < kWaves; ++q) v += *reinterpret_cast<const f32x4*>(&part[q][m][n]);
+        const int row = lo + t0 + mt * 16 + m, id = adapters.of_row[row];
+        if (id >= 0) v += low_rank_of_four<DT>(adapters, row, id, expert, col0 + n, Nout);
+        const u32x2 o = {Elem16<DT>::pack2(v[0], v[1]), Elem16<DT>::pack2(v[2], v[3])};
+        *reinterpret_cast<u32x2*>(C + static_cast<int64_t>(row) * Nout + col0 + n) = o;
+      }
+    }
+  };
+  for (int t0 = 0; t0 < cnt; t0 += 64) {
+    const int rows = min(64, cnt - t0);
+    if (t0 > 0) __syncthreads();
+    if (rows > 32) pass(t0, rows, std::integral_constant<int, 4>{});
+    else if (rows > 16) pass(t0, rows, std::integral_constant<int, 2>{});
+    else pass(t0, rows, std::integral_constant<int, 1>{});
+  }
+}
+
+}  // namespace few_by_rows
+
 // The weight gradients C[i][m, n] = sum_{r in expert i} A[r, m] * B[r, n] on 256 x 256 tiles: persistent, one block per CU,
 // the K loop of gemm_core.h with both operands by rows; a tile's first two k-tiles are requested before the previous
 // tile's epilogue.  k-rows past the expert's last one read zeros (the descriptors end there).
@@ -610,9 +729,20 @@ hipError_t launch_data_gradient(int dtype, const bf16_t* a, const bf16_t* b, bf1
                                 const AdapterRows* adapters) {
   using namespace bwd;
   if (rows == 0) return hipSuccess;
+  const int n_cus = cus_of_current_device() & ~7;
+  const int64_t small_tiles = ((rows + 127) / 128 + n_exp) * ((n + 127) / 128);   // tiles of 128 x 128, at most
+  // (With adapters, few rows of few tiles: the kernel of few rows.  dx of 16 rows of 2048 from 2048, 8 experts: 34 us on tiles, 12 on
+  // that kernel; 64 rows, one expert: 32 and 14; one row of 2048 from 8192, 8 experts: 27 and 21; 128 rows, 1024 from 4096, one expert: 46
+  // and 45.  Tiles for every CU stream the weights as fast: 128 rows, 32 experts 205 and 224 us; and more rows of an expert are further
+  // passes over its weights: 130 of 8192 from 8192: 76 and 105.)
+  if (adapters != nullptr && rows <= 128 && rows <= 64 * static_cast<int64_t>(n_exp) && small_tiles < n_cus) {
+    const unsigned blocks = static_cast<unsigned>(n_exp * ((n + few_by_rows::kColumns - 1) / few_by_rows::kColumns));
+    if (dtype == MOE_F16) few_by_rows::data_gradient_few_rows_kernel<MOE_F16><<<blocks, 64 * few_by_rows::kWaves, 0, s>>>(a, b, cc, offsets, n, k, *adapters);
+    else few_by_rows::data_gradient_few_rows_kernel<MOE_BF16><<<blocks, 64 * few_by_rows::kWaves, 0, s>>>(a, b, cc, offsets, n, k, *adapters);
+    return hipGetLastError();
+  }
   hipError_t e = ensure_backward_attrs();
   if (e != hipSuccess) return e;
-  const int n_cus = cus_of_current_device() & ~7;
   auto few = [&](int64_t r) { return 2 * ((r + 255) / 256 + n_exp) * ((n + 255) / 256) < n_cus; };
   // (With adapters also few tiles of a long contraction, which that kernel cuts between CUs.  301 rows of 1024 from 4096: 62 us on
   // the small tiles, 54 on the large; 130 of 8192 from 8192: 117 and 76; but 300 of 4096 from 1024: 24 and 36, and 64 of 2048 from 2048 31
@@ -625,7 +755,7 @@ hipError_t launch_data_gradient(int dtype, const bf16_t* a, const bf16_t* b, bf1
     if (e != hipSuccess || pick_cus == 0) return e;
   }
   // (as a second shape it has fewer than n_cus / 2 tiles of 256 x 256 to do, each four of its own)
-  const int64_t tiles = big ? 2 * n_cus : ((rows + 127) / 128 + n_exp) * ((n + 127) / 128);
+  const int64_t tiles = big ? 2 * n_cus : small_tiles;
   const unsigned grid = static_cast<unsigned>((tiles + 7) / 8 * 8);
   const AdapterRows ad = adapters != nullptr ? *adapters : AdapterRows{};
 #define PPMOE_LAUNCH(DT, ADAPT) \

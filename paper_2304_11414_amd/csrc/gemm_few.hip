@@ -18,7 +18,7 @@
 
 #include <type_traits>
 
-#include "common.h"
+#include "adapter_core.h"
 
 namespace ppmoe {
 
@@ -65,29 +65,7 @@ __global__ __launch_bounds__(kThreads, 4) void grouped_gemm_few_rows_kernel(
   auto store = [&](int row, int n, f32x4 v) __attribute__((always_inline)) {
     if constexpr (ADAPT) {
       const int a = adapters.of_row[row];
-      if (a >= 0) {
-        const u32x4* low = reinterpret_cast<const u32x4*>(adapters.low + static_cast<int64_t>(row) * adapters.rank);
-        const u32x4* up = reinterpret_cast<const u32x4*>(
-            adapters.up + ((static_cast<int64_t>(a) * adapters.n_exp + expert) * Nout + col0 + n) * adapters.rank);
-        const int pieces = adapters.rank >> 3;
-        f32x4 more = {0.f, 0.f, 0.f, 0.f};
-#pragma clang loop unroll(disable)
-        for (int p = 0; p < pieces; ++p) {
-          const u32x4 l = low[p];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const u32x4 u = up[i * pieces + p];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              float l0, l1, u0, u1;
-              Elem16<DT>::widen2(l[q], l0, l1);
-              Elem16<DT>::widen2(u[q], u0, u1);
-              more[i] = fmaf(l1, u1, fmaf(l0, u0, more[i]));
-            }
-          }
-        }
-        v += more;
-      }
+      if (a >= 0) v += low_rank_of_four<DT>(adapters, row, a, expert, col0 + n, Nout);
     }
     if (GELU) v = gelu_tanh4(v);
     bf16_t* base = C;
