@@ -308,10 +308,12 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_bwd_kernel(
 
 // The data gradient on few rows, with the rows' adapters:  C[r, n] = sum_k A[r, k] * B[i][k, n] (+ adapter_core.h).
 //
-// One pass over the weights per 64 rows of an expert, bound by their stream.  A block owns 64 columns of one expert, 128 bytes of each of B's rows;
-// its eight wavefronts split the contraction, 64 of B's rows at a time each: those go through LDS of the wavefront's own (4 KiB a
-// step of 32) and from there across the rows into operands (transposing read), A's rows come straight from memory.  The partial sums meet
-// in LDS, 16 rows at a time, and are added in wavefront order.
+// A block owns 64 rows and 64 columns of one expert, 128 bytes of each of B's rows; the blocks of an expert's other rows read those through
+// the caches.  Its eight wavefronts split the contraction, 64 of B's rows at a time each (32 with more than 32 rows of A): those go through LDS
+// of the wavefront's own (4 KiB a step of 32) and from there across the rows into operands (transposing read); A's rows come straight from
+// memory; the next step's loads are under way meanwhile.  The partial sums meet in LDS, 16 rows at a time, and are added in wavefront
+// order.  Bound by the latency of a wavefront's chain of steps (k / 512 of them, 2 to 3 us each 8: 15 us for k 2048, 25 for 4096), with more
+// blocks than CUs by the weights' stream.
 namespace few_by_rows {
 
 constexpr int kWaves = 8, kColumns = 64, kLd = kColumns + 4;
@@ -414,13 +416,11 @@ __global__ __launch_bounds__(64 * kWaves) void data_gradient_few_rows_kernel(con
       }
     }
   };
-  for (int t0 = 0; t0 < cnt; t0 += 64) {
-    const int rows = min(64, cnt - t0);
-    if (t0 > 0) __syncthreads();
-    if (rows > 32) pass(t0, rows, std::integral_constant<int, 4>{});
-    else if (rows > 16) pass(t0, rows, std::integral_constant<int, 2>{});
-    else pass(t0, rows, std::integral_constant<int, 1>{});
-  }
+  const int t0 = blockIdx.y * 64, rows = min(64, cnt - t0);
+  if (rows <= 0) return;
+  if (rows > 32) pass(t0, rows, std::integral_constant<int, 4>{});
+  else if (rows > 16) pass(t0, rows, std::integral_constant<int, 2>{});
+  else pass(t0, rows, std::integral_constant<int, 1>{});
 }
 
 }  // namespace few_by_rows
@@ -731,12 +731,11 @@ hipError_t launch_data_gradient(int dtype, const bf16_t* a, const bf16_t* b, bf1
   if (rows == 0) return hipSuccess;
   const int n_cus = cus_of_current_device() & ~7;
   const int64_t small_tiles = ((rows + 127) / 128 + n_exp) * ((n + 127) / 128);   // tiles of 128 x 128, at most
-  // (With adapters, few rows of few tiles: the kernel of few rows.  dx of 16 rows of 2048 from 2048, 8 experts: 34 us on tiles, 12 on
-  // that kernel; 64 rows, one expert: 32 and 14; one row of 2048 from 8192, 8 experts: 27 and 21; 128 rows, 1024 from 4096, one expert: 46
-  // and 45.  Tiles for every CU stream the weights as fast: 128 rows, 32 experts 205 and 224 us; and more rows of an expert are further
-  // passes over its weights: 130 of 8192 from 8192: 76 and 105.)
-  if (adapters != nullptr && rows <= 128 && rows <= 64 * static_cast<int64_t>(n_exp) && small_tiles < n_cus) {
-    const unsigned blocks = static_cast<unsigned>(n_exp * ((n + few_by_rows::kColumns - 1) / few_by_rows::kColumns));
+  // (With adapters, tiles for less than two thirds of the CUs: the kernel of few rows.  dx alone, in us, on tiles and there: 64 rows of
+  // 2048 from 2048, 8 experts 32 and 14, one expert 29 and 15; 301 rows of 1024 from 4096 51 and 26, 1000 of 4 experts 53 and 38; 130 of
+  // 8192 from 8192 75 and 67; but past that 2000 rows of 1024 from 1024, 8 experts 23 and 28; 512 of 8192 from 2048 71 and 102.)
+  if (adapters != nullptr && 3 * small_tiles < 2 * n_cus) {
+    const dim3 blocks(static_cast<unsigned>(n_exp * ((n + few_by_rows::kColumns - 1) / few_by_rows::kColumns)), (rows + 63) / 64);
     if (dtype == MOE_F16) few_by_rows::data_gradient_few_rows_kernel<MOE_F16><<<blocks, 64 * few_by_rows::kWaves, 0, s>>>(a, b, cc, offsets, n, k, *adapters);
     else few_by_rows::data_gradient_few_rows_kernel<MOE_BF16><<<blocks, 64 * few_by_rows::kWaves, 0, s>>>(a, b, cc, offsets, n, k, *adapters);
     return hipGetLastError();

@@ -216,6 +216,9 @@ SHAPES = [
     ((1500,), 128, 256, 64, 8, dict(mix="tokens")),                            # every adapter in every tile
     ((2000, 300), 2048, 512, 3, 16, dict(mix="requests")),                     # tiles cut between CUs
     ((400,), 192, 320, 2, 16, dict(mix="none")),
+    ((2000, 300), 4096, 512, 5, 16, dict(mix="tokens")),                       # dx on the large tiles
+    ((600,), 4096, 4096, 3, 24, dict(mix="tokens")),                           # dx on large tiles cut between CUs
+    ((700, 300), 4104, 1000, 3, 32, dict(mix="tokens")),                       # dx, a block per tile
 ]
 
 
@@ -262,7 +265,8 @@ def test_no_rows_give_zero_gradients():
 
 
 @gpu
-@pytest.mark.parametrize("counts,K,N", [((20,), 256, 264), ((300, 50), 136, 264), ((700, 90), 512, 520), ((700, 90), 512, 512)])
+@pytest.mark.parametrize("counts,K,N", [((20,), 256, 264), ((300, 50), 136, 264), ((700, 90), 512, 520), ((700, 90), 512, 512),
+                                          ((600,), 4096, 4096), ((700, 300), 4104, 1000)])
 def test_one_adapters_infinities_stay_with_its_rows(counts, K, N):
     """Rows of other adapters have the bits they have when that adapter is sound; its own rows are NaN where the definition is not
     finite."""
