@@ -7,13 +7,15 @@
  *
  * Conventions that hold for every function below
  *   - Every data pointer is a DEVICE pointer owned by the caller, 16-byte aligned, row-major and
- *     contiguous.  Only `const moe_config*` and `stage_events` arrays are HOST pointers.
+ *     contiguous.  HOST pointers are only the configurations, the `stage_events` arrays, and
+ *     moe_adamw_plan's tensor array and plan.
  *   - `stream` is a hipStream_t passed as void* (NULL = the null stream).  Work is enqueued
  *     asynchronously; nothing here allocates or frees device memory.  Results are valid once the
  *     caller has synchronised the stream.  The calls that SYNCHRONISE the stream are: moe_init;
  *     moe_ffn_check; moe_backward_check; moe_ffn_clock; moe_event_elapsed_ms (on its event); and, once per
  *     device and only if moe_init has not been called for that device, the first call that runs an expert
- *     product (moe_expert_ffn, _up, _down and _backward, the moe_layer_* calls) with bf16/fp16 input --
+ *     product (moe_expert_ffn, _up, _down and _backward, moe_adapter_forward and _backward, the moe_layer_* calls)
+ *     with bf16/fp16 input --
  *     unless that call is made under stream capture, where nothing synchronises (see moe_init).
  *   - Return value: MOE_OK (0) or a negative moe_status.  Arguments are validated on the host
  *     before anything is launched; on error nothing has been enqueued.
@@ -46,7 +48,7 @@ typedef enum {
   MOE_ERR_ALIGN = -4,     /* a device pointer is not 16-byte aligned                 */
   MOE_ERR_WORKSPACE = -5, /* workspace_bytes smaller than moe_workspace_bytes(cfg)   */
   MOE_ERR_HIP = -6,       /* a HIP runtime call (launch, event record) failed        */
-  MOE_ERR_OVERLAP = -7    /* memory that the call would write is named twice         */
+  MOE_ERR_OVERLAP = -7    /* memory that the call would write is named twice (adapters, AdamW) */
 } moe_status;
 
 typedef enum { MOE_F32 = 0, MOE_BF16 = 1, MOE_F16 = 2 } moe_dtype;
@@ -346,9 +348,10 @@ int moe_layer_forward_aux(const moe_config* cfg, const void* x, const void* Wg, 
  *   y[r, :] = u[r, :], or GeLU(u[r, :]) (tanh form) with MOE_ACT_GELU
  * W [n_exp, N, K], A [n_adapters, n_exp, rank, K], B [n_adapters, n_exp, N, rank], x [rows, K], y [rows, N] in dtype (BF16 or
  * F16); scale [n_adapters] float32, or NULL for ones; adapter [tokens], perm [rows], offsets [n_exp + 1] int32; v [rows, rank] float32.
- * All products are accumulated in float32 and y is rounded once.  scale v enters the second product in dtype (so it has to
- * be within an fp16 number's range with F16).  Infinities and NaNs in an adapter's A or B reach rows of that adapter alone (B's as
- * NaN, and up to 31 columns beside them with them); rows without an adapter have the bits they would have without any.
+ * All products are accumulated in float32 and y is rounded once.  scale v, and t of the backward, enter the second product in
+ * dtype (so they have to be within an fp16 number's range with F16).  Infinities and NaNs in an adapter's A or B reach rows of
+ * that adapter alone (B's as NaN, and up to 31 columns beside them with them); rows without an adapter have the bits they would
+ * have without any.
  * rows is the most there are: rows at or beyond offsets[n_exp] are neither read nor written.
  * Limits: rows >= 0, K and N multiples of 8 up to 2^20, n_exp <= 256, n_exp * n_adapters <= 65536, rank a multiple of 8 up to 128,
  * top_k <= 8.
@@ -357,10 +360,12 @@ int moe_layer_forward_aux(const moe_config* cfg, const void* x, const void* Wg, 
  *   dx[r, :] = W[i]^T dy[r, :] + A[a][i]^T t[r, :]              [rows, K] dtype; not computed when dx is NULL
  *   dA[a][i] = sum over its rows of t[r, :] x[r, :]^T              [n_adapters, n_exp, rank, K] float32
  *   dB[a][i] = sum over its rows of dy[r, :] (scale[a] v[r, :])^T   [n_adapters, n_exp, N, rank] float32
- * dA and dB are overwritten in full (zeros for a pair without rows) and hold float32 accuracy: t and v enter as two 16-bit summands.
+ * dA and dB are overwritten in full (zeros for a pair without rows) and hold float32 accuracy: t and v enter as 16-bit summands,
+ * three with BF16, two with F16.  (K + N) * n_exp * n_adapters is at most 2^28 in the backward.
  * Sums have a fixed order: the same bits on every run.  Neither call allocates or, after moe_init, synchronises.
  * workspace: at least moe_adapter_workspace_bytes / moe_adapter_backward_workspace_bytes bytes (0 on an invalid config); calls
- * that share one must be ordered on one stream. */
+ * that share one must be ordered on one stream.  An output or the workspace that overlaps any other array of the call is refused
+ * (MOE_ERR_OVERLAP): neither call works in place. */
 enum { MOE_ACT_NONE = 0, MOE_ACT_GELU = 1 };
 typedef struct {
   int32_t rows, K, N;
@@ -399,7 +404,8 @@ int moe_adapter_backward(const moe_adapter_config* cfg, const void* x, const int
  * moe_adamw_plan_bytes bytes, 0 on invalid arguments) and *n_chunks.  The caller copies the plan to device memory once and
  * keeps it as long as the tensors stay where they are.  Memory that would be written by two tensors, or twice by one, or is the gradient of
  * one and written by another is refused (MOE_ERR_OVERLAP).
- * moe_adamw_step makes the step: plan and values in DEVICE memory, n_tensors and n_chunks as in the plan.  The values are read by the kernel,
+ * moe_adamw_step makes the step: plan and values in DEVICE memory, cfg, n_tensors and n_chunks as in the
+ * plan (with other moment_bits nothing is written).  The values are read by the kernel,
  * so a captured call replays with what they hold then.  skip != 0: nothing is written (a program that
  * found its gradients infinite).  step counts from 1 (less is taken as 1).  Every element is written by one thread: the
  * same bits on every run.  0 <= beta < 1, eps > 0 as a float32. */

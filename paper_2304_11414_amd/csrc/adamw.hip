@@ -42,7 +42,7 @@ struct Entry {
   float* p;
   const float* g;
   void *m, *v;
-  uint8_t *m_power, *v_power;
+  uint8_t *m_power, *v_power;   // NULL with float32 moments
   uint16_t* half;
   int64_t n;
   int32_t first_chunk, half_dtype;
@@ -130,6 +130,7 @@ __global__ __launch_bounds__(kThreads) void adamw_f32_kernel(const Entry* __rest
   const moe_adamw_values s = *values;
   if (s.skip != 0) return;
   const Entry e = entries[of_chunk[blockIdx.x]];
+  if (e.m_power != nullptr) return;   // (a plan of 8-bit moments)
   const Step st = step_of(h, s, e);
   const int64_t begin = static_cast<int64_t>(blockIdx.x - e.first_chunk) * kChunk + threadIdx.x * 4;
   constexpr int kTurns = kChunk / (4 * kThreads);
@@ -237,6 +238,7 @@ __global__ __launch_bounds__(kThreads) void adamw_8bit_kernel(const Entry* __res
   const moe_adamw_values s = *values;
   if (s.skip != 0) return;
   const Entry e = entries[of_chunk[blockIdx.x]];
+  if (e.m_power == nullptr) return;   // (a plan of float32 moments)
   const Step st = step_of(h, s, e);
   const int64_t begin = static_cast<int64_t>(blockIdx.x - e.first_chunk) * kChunk + threadIdx.x * 8;
   constexpr int kTurns = kChunk / (8 * kThreads);
@@ -389,7 +391,8 @@ int moe_adamw_plan(const moe_adamw_config* cfg, const moe_adamw_tensor* tensors,
   int32_t chunk = 0;
   for (int i = 0; i < n_tensors; ++i) {
     const moe_adamw_tensor& t = tensors[i];
-    const adamw::Entry e = {t.p, t.g, t.m, t.v, t.m_power, t.v_power, static_cast<uint16_t*>(t.half), t.n, chunk, t.half_dtype,
+    const bool codes = cfg->moment_bits == 8;
+    const adamw::Entry e = {t.p, t.g, t.m, t.v, codes ? t.m_power : nullptr, codes ? t.v_power : nullptr, static_cast<uint16_t*>(t.half), t.n, chunk, t.half_dtype,
                             t.lr_scale, t.weight_decay};
     memcpy(at + i * sizeof(e), &e, sizeof(e));
     for (int64_t left = t.n; left > 0; left -= adamw::kChunk, ++chunk)

@@ -686,6 +686,29 @@ Layout layout_of(const moe_adapter_config& c, bool backward) {
   return L;
 }
 
+// The backward's launches over pairs and columns stay within what a grid may have.
+int check_backward(const moe_adapter_config* c) {
+  const int st = check_config(c);
+  if (st != MOE_OK) return st;
+  if (c->activation != MOE_ACT_NONE) return MOE_ERR_SHAPE;
+  return (static_cast<int64_t>(c->K) + c->N) * c->n_exp * c->n_adapters > (int64_t(1) << 28) ? MOE_ERR_SHAPE : MOE_OK;
+}
+
+struct Memory {
+  const void* at;   // or NULL
+  size_t bytes;
+};
+// Does one of the first `written` overlap another?
+template <int N>
+bool overlapping(const Memory (&m)[N], int written) {
+  for (int i = 0; i < written; ++i)
+    for (int j = i + 1; j < N; ++j) {
+      const uintptr_t a = reinterpret_cast<uintptr_t>(m[i].at), b = reinterpret_cast<uintptr_t>(m[j].at);
+      if (a != 0 && b != 0 && a < b + m[j].bytes && b < a + m[i].bytes) return true;
+    }
+  return false;
+}
+
 template <int DT>
 hipError_t launch_shrink_of(const ShrinkArgs& a, int64_t rows, hipStream_t s) {
   const int64_t tiles = (rows + a.tile_rows - 1) / a.tile_rows * a.cuts;
@@ -755,7 +778,7 @@ size_t moe_adapter_workspace_bytes(const moe_adapter_config* cfg) {
 }
 
 size_t moe_adapter_backward_workspace_bytes(const moe_adapter_config* cfg) {
-  return adapter::check_config(cfg) == MOE_OK && cfg->activation == MOE_ACT_NONE ? adapter::layout_of(*cfg, true).total : 0;
+  return adapter::check_backward(cfg) == MOE_OK ? adapter::layout_of(*cfg, true).total : 0;
 }
 
 int moe_adapter_forward(const moe_adapter_config* cfg, const void* x, const int32_t* offsets, const void* W, const void* A,
@@ -773,6 +796,11 @@ int moe_adapter_forward(const moe_adapter_config* cfg, const void* x, const int3
     if (adapter::misaligned(p)) return MOE_ERR_ALIGN;
   const adapter::Layout L = adapter::layout_of(*cfg, false);
   if (workspace_bytes < L.total) return MOE_ERR_WORKSPACE;
+  const size_t n_rows = cfg->rows, pairs = static_cast<size_t>(cfg->n_exp) * cfg->n_adapters, k = cfg->K, n = cfg->N, r = cfg->rank;
+  const adapter::Memory memory[] = {{y, n_rows * n * 2}, {v, n_rows * r * 4}, {workspace, L.total}, {x, n_rows * k * 2},
+                                    {offsets, (cfg->n_exp + 1) * size_t(4)}, {W, cfg->n_exp * n * k * 2}, {A, pairs * r * k * 2},
+                                    {B, pairs * n * r * 2}, {scale, cfg->n_adapters * size_t(4)}, {adapter, 4}, {perm, n_rows * 4}};
+  if (adapter::overlapping(memory, 3)) return MOE_ERR_OVERLAP;
   hipStream_t s = static_cast<hipStream_t>(stream);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   int32_t* of_row = reinterpret_cast<int32_t*>(ws + L.of_row);
@@ -790,9 +818,8 @@ int moe_adapter_forward(const moe_adapter_config* cfg, const void* x, const int3
 int moe_adapter_backward(const moe_adapter_config* cfg, const void* x, const int32_t* offsets, const void* W, const void* A,
                          const void* B, const float* scale, const int32_t* adapter, const int32_t* perm, const void* dy,
                          const float* v, void* dx, float* dA, float* dB, void* workspace, size_t workspace_bytes, void* stream) {
-  const int st = adapter::check_config(cfg);
+  const int st = adapter::check_backward(cfg);
   if (st != MOE_OK) return st;
-  if (cfg->activation != MOE_ACT_NONE) return MOE_ERR_SHAPE;
   if (offsets == nullptr || dA == nullptr || dB == nullptr || workspace == nullptr) return MOE_ERR_NULL;
   if (cfg->rows > 0 && (x == nullptr || W == nullptr || A == nullptr || B == nullptr || adapter == nullptr || dy == nullptr || v == nullptr))
     return MOE_ERR_NULL;
@@ -806,6 +833,14 @@ int moe_adapter_backward(const moe_adapter_config* cfg, const void* x, const int
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   const int n_exp = cfg->n_exp, rank = cfg->rank, K = cfg->K, N = cfg->N;
   const int64_t pairs = static_cast<int64_t>(n_exp) * cfg->n_adapters;
+  {
+    const size_t n_rows = cfg->rows, k = K, n = N, a = pairs * rank * k, b = pairs * rank * n;
+    const adapter::Memory memory[] = {{dx, n_rows * k * 2}, {dA, a * 4}, {dB, b * 4}, {workspace, L.total}, {x, n_rows * k * 2},
+                                      {offsets, (n_exp + 1) * size_t(4)}, {W, n_exp * n * k * 2}, {A, a * 2}, {B, b * 2},
+                                      {scale, cfg->n_adapters * size_t(4)}, {adapter, n_rows > 0 ? 4u : 0u}, {perm, n_rows * 4},
+                                      {dy, n_rows * n * 2}, {v, n_rows * rank * 4}};
+    if (adapter::overlapping(memory, 4)) return MOE_ERR_OVERLAP;
+  }
   int32_t* of_row = reinterpret_cast<int32_t*>(ws + L.of_row);
   bf16_t* low = reinterpret_cast<bf16_t*>(ws + L.low);
   float* t = reinterpret_cast<float*>(ws + L.t);

@@ -325,3 +325,15 @@ def test_captured_step_reads_its_values_at_replay_and_other_streams_agree(bits):
         for s, t in zip(a, b):
             for name in s:
                 assert torch.equal(s[name][1], t[name][1]), (step, name)
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_plan_of_other_moments_writes_nothing(bits):
+    a, b = make((5000, 33), bits, "bfloat16", 3), make((5000, 33), bits, "bfloat16", 3)
+    plan = B.moe_adamw_plan(B.make_adamw_config(moment_bits=bits), views(a))
+    B.moe_adamw_step(B.make_adamw_config(moment_bits=40 - bits), plan, B.moe_adamw_scalars(1, 1e-3))
+    torch.cuda.synchronize()
+    for s, t in zip(a, b):
+        for name, (_, whole) in s.items():
+            assert torch.equal(whole, t[name][1]), name

@@ -7,7 +7,7 @@ at most S):
          wavefront and 8 wavefronts (contractions of 2048): 48 roundings, below 2^-18 S.
   y, dx  one rounding of the result, half a step eps / 2 of it; the low-rank summand's factor is rounded once, eps / 2 of its terms (S_low); the float32
          sums 32 + 64 roundings, below 2^-17 S.  GeLU: |GeLU'| <= 1.13 and its own float32 arithmetic, 2^-18 of the argument.
-  dA, dB u as two 16-bit summands: 2^-17 of each term (bf16: 8 bits, then 8 of the rest), t as v; over 2000 rows 32 + 2 * 63 roundings and at most
+  dA, dB u as at least two 16-bit summands: 2^-17 of each term (8 bits, then 8 of the rest), t as v; over 2000 rows 32 + 2 * 63 roundings and at most
          32 pieces: below 2^-16 S; together 2^-15 S."""
 
 import ctypes
@@ -78,6 +78,35 @@ def test_arguments_refused():
     assert lib.moe_adapter_forward(ctypes.byref(gelu), *[p] * 11, need, None) == -2
     empty = B.make_adapter_config(**{**GOOD, "rows": 0})
     assert lib.moe_adapter_forward(ctypes.byref(empty), *[None] * 11, 0, None) == 0
+
+
+def test_overlapping_memory_is_refused():
+    lib, cfg = B.load_library(), B.make_adapter_config(**GOOD)
+    c = ctypes.byref(cfg)
+    MB = 1 << 20
+    for call, need, n, written in ((lib.moe_adapter_forward, lib.moe_adapter_workspace_bytes(c), 11, (8, 9, 10)),
+                                   (lib.moe_adapter_backward, lib.moe_adapter_backward_workspace_bytes(c), 14, (10, 11, 12, 13))):
+        at = [(i + 1) * 1024 * MB for i in range(n)]
+        for w in written:
+            for other in range(n):
+                if other != w:
+                    a = list(at)
+                    a[w] = a[other]
+                    assert call(c, *map(ctypes.c_void_p, a), need, None) == -7, (n, w, other)
+        a = list(at)
+        a[-1] = at[0] - need + 16        # a workspace whose end reaches into x
+        assert call(c, *map(ctypes.c_void_p, a), need, None) == -7
+
+
+def test_backwards_of_more_than_a_grid_holds_are_refused():
+    lib = B.load_library()
+    most = B.make_adapter_config(rows=64, K=2048, N=2048, n_exp=1, n_adapters=65536, rank=128)
+    assert lib.moe_adapter_backward_workspace_bytes(ctypes.byref(most)) > 0
+    more = B.make_adapter_config(rows=64, K=2048, N=2056, n_exp=1, n_adapters=65536, rank=8)
+    p = [ctypes.c_void_p((i + 1) << 44) for i in range(14)]
+    assert lib.moe_adapter_backward_workspace_bytes(ctypes.byref(more)) == 0
+    assert lib.moe_adapter_workspace_bytes(ctypes.byref(more)) > 0
+    assert lib.moe_adapter_backward(ctypes.byref(more), *p, 1 << 43, None) == -2
 
 
 # ---- GPU ---------------------------------------------------------------------------------------------
