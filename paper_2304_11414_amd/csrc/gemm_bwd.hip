@@ -308,12 +308,12 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_bwd_kernel(
 
 // The data gradient on few rows, with the rows' adapters:  C[r, n] = sum_k A[r, k] * B[i][k, n] (+ adapter_core.h).
 //
-// A block owns 64 rows and 64 columns of one expert, 128 bytes of each of B's rows; the blocks of an expert's other rows read those through
-// the caches.  Its eight wavefronts split the contraction, 64 of B's rows at a time each (32 with more than 32 rows of A): those go through LDS
-// of the wavefront's own (4 KiB a step of 32) and from there across the rows into operands (transposing read); A's rows come straight from
-// memory; the next step's loads are under way meanwhile.  The partial sums meet in LDS, 16 rows at a time, and are added in wavefront
-// order.  Bound by the latency of a wavefront's chain of steps (k / 512 of them, 2 to 3 us each 8: 15 us for k 2048, 25 for 4096), with more
-// blocks than CUs by the weights' stream.
+// A block owns up to 64 rows (tile_rows) and 64 columns of one expert, 128 bytes of each of B's rows; the blocks of an expert's other rows read
+// those through the caches.  Its eight wavefronts split the contraction, 32 of B's rows at a time each (128 with 16 rows of A, 64 with
+// 32): those go through LDS of the wavefront's own (4 KiB per 32) and from there across the rows into operands (transposing read); A's rows
+// come straight from memory; the next step's loads are under way meanwhile.  The partial sums meet in LDS, 16 rows at a time, and
+// are added in wavefront order.  Bound by a wavefront's chain of steps, 1.5 us each (301 rows of 1024 from 4096, 32 rows a block: 8 of
+// them, 18 us); with rows of many experts by the weights' stream.
 namespace few_by_rows {
 
 constexpr int kWaves = 8, kColumns = 64, kLd = kColumns + 4;
@@ -321,7 +321,7 @@ constexpr int kWaves = 8, kColumns = 64, kLd = kColumns + 4;
 template <int DT>
 __global__ __launch_bounds__(64 * kWaves) void data_gradient_few_rows_kernel(const bf16_t* __restrict__ A, const bf16_t* __restrict__ B,
                                                                              bf16_t* __restrict__ C, const int32_t* __restrict__ offsets,
-                                                                             int Nout, int K, AdapterRows adapters) {
+                                                                             int Nout, int K, int tile_rows, AdapterRows adapters) {
   typedef typename Elem16<DT>::vec8 vec8;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves * 16 * kLd * 4];
   float (*part)[16][kLd] = reinterpret_cast<float (*)[16][kLd]>(lds);   // (after the loop: the partial sums)
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(64 * kWaves) void data_gradient_few_rows_kernel(con
   const bool in_columns = col0 + wpiece * 8 < Nout;
 
   auto pass = [&](int t0, int rows, auto mt_c) __attribute__((always_inline)) {
-    constexpr int MT = decltype(mt_c)::value, J = MT == 4 ? 1 : 2, kStep = 32 * J;   // (J 2 with MT 4 needs more than 256 registers)
+    constexpr int MT = decltype(mt_c)::value, J = 4 / MT, kStep = 32 * J;   // (the same registers in flight; twice as many spill)
     const bf16_t* arow[MT];
     f32x4 acc[MT][4];
 #pragma unroll
@@ -416,7 +416,7 @@ __global__ __launch_bounds__(64 * kWaves) void data_gradient_few_rows_kernel(con
       }
     }
   };
-  const int t0 = blockIdx.y * 64, rows = min(64, cnt - t0);
+  const int t0 = blockIdx.y * tile_rows, rows = min(tile_rows, cnt - t0);
   if (rows <= 0) return;
   if (rows > 32) pass(t0, rows, std::integral_constant<int, 4>{});
   else if (rows > 16) pass(t0, rows, std::integral_constant<int, 2>{});
@@ -732,12 +732,17 @@ hipError_t launch_data_gradient(int dtype, const bf16_t* a, const bf16_t* b, bf1
   const int n_cus = cus_of_current_device() & ~7;
   const int64_t small_tiles = ((rows + 127) / 128 + n_exp) * ((n + 127) / 128);   // tiles of 128 x 128, at most
   // (With adapters, tiles for less than two thirds of the CUs: the kernel of few rows.  dx alone, in us, on tiles and there: 64 rows of
-  // 2048 from 2048, 8 experts 32 and 14, one expert 29 and 15; 301 rows of 1024 from 4096 51 and 26, 1000 of 4 experts 53 and 38; 130 of
+  // 2048 from 2048, 8 experts 32 and 14, one expert 29 and 7; 301 rows of 1024 from 4096 51 and 18, 1000 of 4 experts 53 and 38; 130 of
   // 8192 from 8192 75 and 67; but past that 2000 rows of 1024 from 1024, 8 experts 23 and 28; 512 of 8192 from 2048 71 and 102.)
   if (adapters != nullptr && 3 * small_tiles < 2 * n_cus) {
-    const dim3 blocks(static_cast<unsigned>(n_exp * ((n + few_by_rows::kColumns - 1) / few_by_rows::kColumns)), (rows + 63) / 64);
-    if (dtype == MOE_F16) few_by_rows::data_gradient_few_rows_kernel<MOE_F16><<<blocks, 64 * few_by_rows::kWaves, 0, s>>>(a, b, cc, offsets, n, k, *adapters);
-    else few_by_rows::data_gradient_few_rows_kernel<MOE_BF16><<<blocks, 64 * few_by_rows::kWaves, 0, s>>>(a, b, cc, offsets, n, k, *adapters);
+    // (Rows of a block: fewer while every block has a CU.  64, 32 and 16 rows a block: 301 rows of 1024 from 4096 26, 18 and 23 us; 128 rows
+    // 24, 16 and 12; 512 rows of 2048 from 2048 18, 20 and 29.)
+    const int64_t columns = (n + few_by_rows::kColumns - 1) / few_by_rows::kColumns;
+    int tile_rows = 64;
+    while (tile_rows > 16 && ((rows + tile_rows / 2 - 1) / (tile_rows / 2) + n_exp - 1) * columns <= n_cus) tile_rows /= 2;
+    const dim3 blocks(static_cast<unsigned>(n_exp * columns), static_cast<unsigned>((rows + tile_rows - 1) / tile_rows));
+    if (dtype == MOE_F16) few_by_rows::data_gradient_few_rows_kernel<MOE_F16><<<blocks, 64 * few_by_rows::kWaves, 0, s>>>(a, b, cc, offsets, n, k, tile_rows, *adapters);
+    else few_by_rows::data_gradient_few_rows_kernel<MOE_BF16><<<blocks, 64 * few_by_rows::kWaves, 0, s>>>(a, b, cc, offsets, n, k, tile_rows, *adapters);
     return hipGetLastError();
   }
   hipError_t e = ensure_backward_attrs();
