@@ -748,9 +748,9 @@ hipError_t launch_data_gradient(int dtype, const bf16_t* a, const bf16_t* b, bf1
   hipError_t e = ensure_backward_attrs();
   if (e != hipSuccess) return e;
   auto few = [&](int64_t r) { return 2 * ((r + 255) / 256 + n_exp) * ((n + 255) / 256) < n_cus; };
-  // (With adapters also few tiles of a long contraction, which that kernel cuts between CUs.  301 rows of 1024 from 4096: 62 us on
-  // the small tiles, 54 on the large; 130 of 8192 from 8192: 117 and 76; but 300 of 4096 from 1024: 24 and 36, and 64 of 2048 from 2048 31
-  // and 30.)
+  // (With adapters also few tiles of a long contraction, which that kernel cuts between CUs.  Small tiles and large, us: 600 rows of 4096 from
+  // 4096 64 and 56; 300 of 8192 from 8192 121 and 83; 500 of 1024 from 8192, 24 experts 146 and 103; but 600 of 4096 from 2048 36 and 55, from
+  // 1024 21 and 35.)
   const bool big = k % BK == 0 && k < (1 << 22) && n < kColumnsByRows && (!few(rows) || (adapters != nullptr && k >= 4096));
   const int pick_cus = big && expected_rows < rows && few(expected_rows) ? n_cus : 0;
   if (big) {
