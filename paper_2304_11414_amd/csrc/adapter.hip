@@ -58,6 +58,9 @@ __device__ __forceinline__ void store_low_rank(const ShrinkArgs& a, int64_t at, 
   *reinterpret_cast<u32x2*>(a.low + at) = o;
 }
 
+template <int MR, int WAVES, int G>
+constexpr int kPartBytes = sizeof(float) * WAVES * 16 * G * (16 * MR + 4);
+
 // MR: blocks of 16 of the rank; J: k-steps of 32 fetched at a time
 template <int DT, int MR, int WAVES, int G, int J>
 __global__ __launch_bounds__(64 * WAVES) void shrink_kernel(ShrinkArgs a) {
@@ -79,17 +82,40 @@ __global__ __launch_bounds__(64 * WAVES) void shrink_kernel(ShrinkArgs a) {
   constexpr int kStretch = WAVES * 32 * J;
   const int stretches = (a.K + kStretch - 1) / kStretch;
   const int k_end = min(a.K, (cut + 1) * stretches / a.cuts * kStretch), k_begin = cut * stretches / a.cuts * kStretch;
-  int r[G];
+  // Two k-steps of 16 rows are fetched as eight rows of 128 bytes each, whole lines (rows may be a power of two apart, and then one line of each
+  // of 16 rows is more than their set of the cache holds until its other half is asked for), and change places in LDS of the
+  // wavefront's own.  One k-step (J 1) comes as the operand is.
+  constexpr bool kLines = J % 2 == 0;
+  unsigned char* own = reinterpret_cast<unsigned char*>(shrink_lds) + kPartBytes<MR, WAVES, G> + wave * 2048;
+  auto row_at = [&](int j) __attribute__((always_inline)) -> int { return kLines ? (j & 1) * 8 + (lane >> 3) : fr; };   // of 16
+  auto k_at = [&](int j) __attribute__((always_inline)) -> int { return kLines ? (j >> 1) * 64 + (lane & 7) * 8 : 32 * j + fq * 8; };
+  auto settle = [&](auto& v) __attribute__((always_inline)) {
+    if constexpr (kLines) {
+      constexpr int N = sizeof(v[0]) / sizeof(u32x4);
 #pragma unroll
-  for (int g = 0; g < G; ++g) r[g] = lo + row0 + min(g * 16 + fr, count - 1);
+      for (int j = 0; j < J; j += 2)
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int row = row_at(h);
+            *reinterpret_cast<u32x4*>(own + row * 128 + (((lane & 7) ^ (row & 7)) << 4)) = v[j + h][n];
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) v[j + h][n] = *reinterpret_cast<const u32x4*>(own + fr * 128 + (((h * 4 + fq) ^ (fr & 7)) << 4));
+        }
+    }
+  };
   const u32x4 zero = u32x4{0u, 0u, 0u, 0u};
   u32x4 x[J][G];
   auto load_x = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int g = 0; g < G; ++g)
-        x[j][g] = k0 + 32 * j + fq * 8 < k_end ? *reinterpret_cast<const u32x4*>(a.x + static_cast<int64_t>(r[g]) * a.K + k0 + 32 * j + fq * 8) : zero;
+      for (int g = 0; g < G; ++g) {
+        const int row = lo + row0 + min(g * 16 + row_at(j), count - 1);
+        x[j][g] = k0 + k_at(j) < k_end ? *reinterpret_cast<const u32x4*>(a.x + static_cast<int64_t>(row) * a.K + k0 + k_at(j)) : zero;
+      }
   };
   int k0 = k_begin + wave * 32 * J;
   load_x(k0);   // (on their way while the pairs are looked up)
@@ -117,13 +143,13 @@ __global__ __launch_bounds__(64 * WAVES) void shrink_kernel(ShrinkArgs a) {
   const int first = __builtin_amdgcn_readfirstlane(least_above(mine, -1));
   // (the next pair's, or stretch's, operand is on its way while this one's is multiplied)
   auto load_w = [&](u32x4 (&w)[J][MR], int pair, int k) __attribute__((always_inline)) {
-    const bf16_t* m = a.m + static_cast<int64_t>(pair) * a.rank * a.K + k + fq * 8;
+    const bf16_t* m = a.m + static_cast<int64_t>(pair) * a.rank * a.K + k;
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
       for (int mr = 0; mr < MR; ++mr)   // (rows past the rank re-read the last one; their sums are not stored)
-        w[j][mr] = k + 32 * j + fq * 8 < k_end
-                       ? *reinterpret_cast<const u32x4*>(m + static_cast<int64_t>(min(mr * 16 + fr, a.rank - 1)) * a.K + 32 * j)
+        w[j][mr] = k + k_at(j) < k_end
+                       ? *reinterpret_cast<const u32x4*>(m + static_cast<int64_t>(min(mr * 16 + row_at(j), a.rank - 1)) * a.K + k_at(j))
                        : zero;
   };
   auto multiply = [&](const u32x4 (&w)[J][MR], int pair) __attribute__((always_inline)) {
@@ -146,6 +172,7 @@ __global__ __launch_bounds__(64 * WAVES) void shrink_kernel(ShrinkArgs a) {
   if (first != kNone && k0 < k_end) {
     u32x4 w0[J][MR], w1[J][MR];
     int pair = first, now;
+    bool fresh = true;   // x has been asked for
     load_w(w0, pair, k0);
     // what follows (pair, k0): the next pair of the same stretch, or the first one of the next
     auto turn = [&](u32x4 (&w)[J][MR], u32x4 (&other)[J][MR]) __attribute__((always_inline)) -> bool {
@@ -159,8 +186,11 @@ __global__ __launch_bounds__(64 * WAVES) void shrink_kernel(ShrinkArgs a) {
       const bool more = k0 < k_end;
       if (more) load_w(other, pair, k0);
       __builtin_amdgcn_sched_barrier(0);
+      if (fresh) settle(x);
+      settle(w);
       multiply(w, now);
-      if (more && !same) load_x(k0);
+      fresh = more && !same;
+      if (fresh) load_x(k0);
       return more;
     };
     while (turn(w0, w1) && turn(w1, w0)) {
@@ -719,7 +749,7 @@ hipError_t launch_shrink_of(const ShrinkArgs& a, int64_t rows, hipStream_t s) {
   const unsigned grid = static_cast<unsigned>((tiles + 7) / 8 * 8);   // (every XCD the same run of tiles)
 #define PPMOE_SHRINK(MR, WAVES, G, J)                                                                      \
   do {                                                                                                     \
-    constexpr int kLds = sizeof(float) * WAVES * 16 * G * (16 * MR + 4);                                   \
+    constexpr int kLds = kPartBytes<MR, WAVES, G> + WAVES * 2048;                                          \
     if (kLds > 65536) {                                                                                    \
       static std::atomic<uint64_t> done{0};                                                                \
       const hipError_t e = once_per_device(done, [] {                                                      \
@@ -732,12 +762,10 @@ hipError_t launch_shrink_of(const ShrinkArgs& a, int64_t rows, hipStream_t s) {
   } while (0)
   if (a.tile_rows > 32) {
     if (a.rank <= 64) PPMOE_SHRINK(4, 8, 4, 2);
-    else PPMOE_SHRINK(8, 4, 4, 1);
-  } else if (a.tile_rows > 16) {
+    else PPMOE_SHRINK(8, 4, 4, 2);
+  } else if (a.tile_rows > 16) {   // (ranks up to 32 alone: shape_of_shrink)
     if (a.rank <= 16) PPMOE_SHRINK(1, 8, 2, 4);
-    else if (a.rank <= 32) PPMOE_SHRINK(2, 8, 2, 4);
-    else if (a.rank <= 64) PPMOE_SHRINK(4, 8, 2, 2);
-    else PPMOE_SHRINK(8, 8, 2, 2);
+    else PPMOE_SHRINK(2, 8, 2, 4);
   } else if (a.rank <= 16) PPMOE_SHRINK(1, 8, 1, 8);
   else if (a.rank <= 32) PPMOE_SHRINK(2, 8, 1, 4);
   else if (a.rank <= 64) PPMOE_SHRINK(4, 8, 1, 4);

@@ -341,11 +341,13 @@ __global__ __launch_bounds__(64 * kWaves) void data_gradient_few_rows_kernel(con
 
   auto pass = [&](int t0, int rows, auto mt_c) __attribute__((always_inline)) {
     constexpr int MT = decltype(mt_c)::value, J = 4 / MT, kStep = 32 * J;   // (the same registers in flight; twice as many spill)
-    const bf16_t* arow[MT];
+    // A's rows: two k-steps as whole lines, as the weights are, one (MT 4) as the operand is
+    constexpr bool kLines = J % 2 == 0;
+    auto row_at = [&](int j) __attribute__((always_inline)) -> int { return kLines ? (j & 1) * 8 + wrow : fr; };   // of 16
+    auto k_at = [&](int j) __attribute__((always_inline)) -> int { return kLines ? (j >> 1) * 64 + wpiece * 8 : j * 32 + fq * 8; };
     f32x4 acc[MT][4];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      arow[mt] = A + static_cast<int64_t>(lo + t0 + min(mt * 16 + fr, rows - 1)) * K + fq * 8;   // (rows past the end re-read the last one)
 #pragma unroll
       for (int nt = 0; nt < 4; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -360,7 +362,8 @@ __global__ __launch_bounds__(64 * kWaves) void data_gradient_few_rows_kernel(con
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
-          x[j][mt] = k0 + j * 32 + fq * 8 < K ? *reinterpret_cast<const u32x4*>(arow[mt] + k0 + j * 32) : zero;
+          x[j][mt] = k0 + k_at(j) < K ? *reinterpret_cast<const u32x4*>(A + static_cast<int64_t>(lo + t0 + min(mt * 16 + row_at(j), rows - 1)) * K + k0 + k_at(j))
+                                      : zero;   // (rows past the end re-read the last one)
       }
     };
     load(wave * kStep);
@@ -381,8 +384,22 @@ __global__ __launch_bounds__(64 * kWaves) void data_gradient_few_rows_kernel(con
           core::lds_read_transposed<0>(b[j][nt][0], at);
           core::lds_read_transposed<512>(b[j][nt][1], at);
         }
+        if constexpr (!kLines) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) a[j][mt] = x[j][mt];
+          for (int mt = 0; mt < MT; ++mt) a[j][mt] = x[j][mt];
+        }
+      }
+      if constexpr (kLines) {
+#pragma unroll
+        for (int j = 0; j < J; j += 2)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              *reinterpret_cast<u32x4*>(mine + row_at(h) * 128 + ((wpiece ^ (row_at(h) & 7)) << 4)) = x[j + h][mt];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) a[j + h][mt] = *reinterpret_cast<const u32x4*>(mine + fr * 128 + (((h * 4 + fq) ^ (fr & 7)) << 4));
+          }
       }
       if (k0 + kWaves * kStep < K) load(k0 + kWaves * kStep);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
