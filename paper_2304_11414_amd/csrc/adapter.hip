@@ -30,9 +30,9 @@ constexpr int kMaxColumns = 1 << 20;
 //
 // What bounds it is what a CU fetches, x and the pairs' matrices: (16 G + rank) K elements per block of one pair.  Ranks
 // above 32 take 64 rows a block, and where that leaves CUs without one the contraction is cut between blocks as well, whose partial sums
-// another launch adds (combine_kernel).  Measured: 8192 rows of 2048, 24 requests over 8 experts, rank 32 31 us (34 MB of x, 17 of A: 1.6 TB/s,
-// a chain of loads per pair and stretch; 16 rows a block 35); 8192 rows of 2048, rank 16 18; 4096 rows of 8192, rank 64, cut in four 29 and 5
-// (2.3 TB/s); one row of 2048 5.
+// another launch adds (combine_kernel).  Measured: 8192 rows of 2048, 24 requests over 8 experts, rank 32 22 us (34 MB of x, 17 of A: 2.3 TB/s;
+// 30 with operands fetched by half lines; 8 of them without any adapter; a step per pair and stretch, each a fetch); 8192 rows of 2048,
+// rank 16 14; 4096 rows of 8192, rank 64, cut in four 22 and 6 (3 TB/s); one row of 2048 5.
 struct ShrinkArgs {
   const bf16_t* x;        // [rows, K]
   const bf16_t* m;        // [n_adapters, n_exp, rank, K]
@@ -666,18 +666,21 @@ int64_t most_pieces(const moe_adapter_config& c, int C) {
 // A pair of several pieces has more rows than one piece: at most two slots per full piece.
 int64_t most_slots(const moe_adapter_config& c, int C) { return 2 * (static_cast<int64_t>(c.rows) / rows_of_piece(c, C)) + 1; }
 
-// Rows of a block and cuts of the contraction: 32 rows (64 at ranks above 32), or fewer while that leaves CUs without a block (a
-// row's own adapter is a block's whole work then), down to 16 where the matrices weigh more than the rows and the contraction can be cut.
+// Rows of a block and cuts of the contraction.  Ranks above 32 with more than 512 rows: 64 rows, as the matrices weigh as much as the rows,
+// and the contraction cut, down to a stretch of the block's wavefronts, while that leaves CUs without a block (1000 rows of 2048 to 8192, rank
+// 128, whole forward: 93 us with shares of 1024 and more, 83 with these).  Otherwise 32 rows, and fewer while that leaves CUs without a block, down
+// to one: a row's own adapter is a block's whole work then (300 rows of 1024, rank 64: 45 us the forward, 48 with 64 rows a block).
 void shape_of_shrink(int64_t rows, int rank, int K, int* tile_rows, int* cuts) {
-  int t = rank > 32 ? 64 : 32;
-  const int least = rank > 32 && rows > 512 ? 16 : 1;
   *cuts = 1;
-  while (t > 16 && (rows + t / 2 - 1) / (t / 2) <= 256 && !(rank > 32 && rows > 512)) t /= 2;
-  while (t <= 16 && t > least && (rows + t / 2 - 1) / (t / 2) <= 256) t /= 2;
   if (rank > 32 && rows > 512) {
-    const int64_t tiles = (rows + t - 1) / t;
-    while (*cuts < 8 && tiles * *cuts * 2 <= 256 && K / (*cuts * 2) >= 1024) *cuts *= 2;
+    const int64_t tiles = (rows + 63) / 64;
+    const int stretch = rank > 64 ? 256 : 512;
+    *tile_rows = 64;
+    while (*cuts < 8 && tiles * *cuts * 2 <= 256 && K / (*cuts * 2) >= stretch) *cuts *= 2;
+    return;
   }
+  int t = 32;
+  while (t > 1 && (rows + t / 2 - 1) / (t / 2) <= 256) t /= 2;
   *tile_rows = t;
 }
 
