@@ -40,7 +40,7 @@ struct ShrinkArgs {
   const float* scale;     // [n_adapters] or NULL
   int32_t* of_row;        // out: the adapter of each packed row, or -1
   float* wide;            // out [rows, rank]
-  bf16_t* low;            // out [rows, rank]: scaled, in 16 bits
+  bf16_t* low;            // out [rows, 2 rank]: scaled, as two 16-bit summands
   int n_exp, n_adapters, top_k, K, rank, tile_rows;
   bool scale_wide;        // wide is scaled as well
   int32_t* ticket;        // of count_kernel, set to 0; or NULL
@@ -48,14 +48,26 @@ struct ShrinkArgs {
   int cuts, rows;
 };
 
-// (low in 16 bits: an operand of the matrix instruction that adds the low-rank part.  A rounding of each of `rank` terms, as
-// far off as the one rounding of the result is, and only of the low-rank part.)
+// (low: an operand of the matrix instruction that adds the low-rank part, as two summands, the rounding to 16 bits and that of what it
+// leaves, a row's first ones before its second ones: together 16 bits (bf16) or 22, so that the result is as good as rounded once.)
 template <int DT>
-__device__ __forceinline__ void store_low_rank(const ShrinkArgs& a, int64_t at, f32x4 v, float scale) {
+__device__ __forceinline__ void store_low_rank(const ShrinkArgs& a, int64_t row, int j, f32x4 v, float scale) {
   const f32x4 scaled = v * scale;
-  *reinterpret_cast<f32x4*>(a.wide + at) = a.scale_wide ? scaled : v;
-  const u32x2 o = {Elem16<DT>::pack2(scaled[0], scaled[1]), Elem16<DT>::pack2(scaled[2], scaled[3])};
-  *reinterpret_cast<u32x2*>(a.low + at) = o;
+  *reinterpret_cast<f32x4*>(a.wide + row * a.rank + j) = a.scale_wide ? scaled : v;
+  f32x4 rest = scaled;
+#pragma unroll
+  for (int part = 0; part < 2; ++part) {
+    const u32x2 o = {Elem16<DT>::pack2(rest[0], rest[1]), Elem16<DT>::pack2(rest[2], rest[3])};
+    *reinterpret_cast<u32x2*>(a.low + (row * 2 + part) * a.rank + j) = o;
+    float h[4];
+    Elem16<DT>::widen2(o[0], h[0], h[1]);
+    Elem16<DT>::widen2(o[1], h[2], h[3]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      rest[e] -= h[e];
+      if (!(fabsf(rest[e]) < 3.0e38f)) rest[e] = 0.f;   // (an infinity or a NaN is in the first summand whole)
+    }
+  }
 }
 
 template <int MR, int WAVES, int G>
@@ -206,9 +218,9 @@ __global__ __launch_bounds__(64 * WAVES) void shrink_kernel(ShrinkArgs a) {
     f32x4 v = *reinterpret_cast<const f32x4*>(&part[0][q][j]);
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) v += *reinterpret_cast<const f32x4*>(&part[w][q][j]);
-    const int64_t at = static_cast<int64_t>(lo + row0 + q) * a.rank + j;
-    if (a.cuts > 1) *reinterpret_cast<f32x4*>(a.partial + cut * static_cast<int64_t>(a.rows) * a.rank + at) = v;
-    else store_low_rank<DT>(a, at, v, row_scale[q]);
+    const int64_t row = lo + row0 + q;
+    if (a.cuts > 1) *reinterpret_cast<f32x4*>(a.partial + (cut * static_cast<int64_t>(a.rows) + row) * a.rank + j) = v;
+    else store_low_rank<DT>(a, row, j, v, row_scale[q]);
   }
 }
 
@@ -218,11 +230,13 @@ __global__ __launch_bounds__(256) void combine_kernel(ShrinkArgs a) {
   const int lo = a.offsets[0], quads = a.rank / 4;
   const int64_t total = static_cast<int64_t>(a.offsets[a.n_exp] - lo) * quads;
   for (int64_t p = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; p < total; p += static_cast<int64_t>(gridDim.x) * 256) {
-    const int64_t row = lo + p / quads, at = row * a.rank + (p % quads) * 4;
+    const int64_t row = lo + p / quads;
+    const int j = static_cast<int>(p % quads) * 4;
+    const int64_t at = row * a.rank + j;
     f32x4 v = *reinterpret_cast<const f32x4*>(a.partial + at);
     for (int cut = 1; cut < a.cuts; ++cut) v += *reinterpret_cast<const f32x4*>(a.partial + cut * static_cast<int64_t>(a.rows) * a.rank + at);
     const int id = a.of_row[row];
-    store_low_rank<DT>(a, at, v, id >= 0 && a.scale != nullptr ? a.scale[id] : 1.f);
+    store_low_rank<DT>(a, row, j, v, id >= 0 && a.scale != nullptr ? a.scale[id] : 1.f);
   }
 }
 
@@ -699,7 +713,7 @@ Layout layout_of(const moe_adapter_config& c, bool backward) {
   };
   const size_t rows = c.rows, pairs = static_cast<size_t>(c.n_exp) * c.n_adapters;
   L.of_row = take(rows * 4);
-  L.low = take(rows * c.rank * 2);
+  L.low = take(rows * c.rank * 4);
   L.gemm = take(grouped_gemm_workspace_bytes());
   int tile_rows = 0, cuts = 1;
   shape_of_shrink(c.rows, c.rank, backward ? c.N : c.K, &tile_rows, &cuts);
@@ -844,7 +858,7 @@ int moe_adapter_forward(const moe_adapter_config* cfg, const void* x, const int3
                            cfg->n_exp, cfg->n_adapters, cfg->top_k, cfg->K, cfg->rank, 0, false, nullptr, reinterpret_cast<float*>(ws + L.cut), 1, 0};
   hipError_t e = adapter::launch_shrink(cfg->dtype, a, cfg->rows, s);
   if (e != hipSuccess) return MOE_ERR_HIP;
-  const AdapterRows rows = {of_row, low, static_cast<const bf16_t*>(B), cfg->n_exp, cfg->rank};
+  const AdapterRows rows = {of_row, low, v, scale, static_cast<const bf16_t*>(B), cfg->n_exp, cfg->rank};
   e = launch_grouped_gemm(cfg->dtype, cfg->activation == MOE_ACT_GELU, x, W, y, offsets, cfg->n_exp, cfg->rows, cfg->N, cfg->K,
                           ws + L.gemm, s, 0, nullptr, nullptr, 1, nullptr, nullptr, &rows);
   return e == hipSuccess ? MOE_OK : MOE_ERR_HIP;
@@ -891,7 +905,7 @@ int moe_adapter_backward(const moe_adapter_config* cfg, const void* x, const int
     e = adapter::launch_shrink(cfg->dtype, a, cfg->rows, s);
     if (e != hipSuccess) return MOE_ERR_HIP;
     if (dx != nullptr) {
-      const AdapterRows rows = {of_row, low, At, n_exp, rank};
+      const AdapterRows rows = {of_row, low, t, nullptr, At, n_exp, rank};
       e = launch_data_gradient(cfg->dtype, static_cast<const bf16_t*>(dy), static_cast<const bf16_t*>(W), static_cast<bf16_t*>(dx),
                                offsets, n_exp, cfg->rows, cfg->rows, K, N, ws + L.gemm, s, &rows);
       if (e != hipSuccess) return MOE_ERR_HIP;

@@ -2,8 +2,9 @@
 //
 //   C[r, n] += sum_j low[r, j] * up[a][i][n, j],   a the adapter of packed row r (none: nothing), i the expert, j < rank
 //
-// low [rows, rank] 16-bit (scaled already), up [n_adapters, n_exp, Nout, rank] 16-bit.  rank is a multiple of 8, so an adapter is
-// rank / 8 pieces of 16 bytes per row of either matrix: what a lane holds of a matrix instruction's operand.  A
+// low [rows, 2 rank] 16-bit: each row's factor, scaled already, as two summands (the kernels of few rows read the float32 that they stand
+// for), up [n_adapters, n_exp, Nout, rank] 16-bit.  rank is a multiple of 8, so an adapter is rank / 8 pieces of 16 bytes per row of `up`, twice as
+// many per row of `low`: what a lane holds of a matrix instruction's operand.  Both summands meet the same pieces of `up`.  A
 // wavefront goes through the adapters that its rows have, in ascending order; a row's operand is zero where it has another
 // one.  Both operands come straight from memory: it is a step or two per tile where the rows are whole requests, next to the 32 of a
 // contraction of 1024.
@@ -39,29 +40,29 @@ __device__ __forceinline__ int least_above(const int (&mine)[MI], int a) {
   return min(least, __builtin_amdgcn_update_dpp(0, least, 0x121, 0xf, 0xf, true));
 }
 
-// The kernels of few rows: four columns from `col` on of packed row `row`, which has adapter a >= 0.
+// The kernels of few rows: four columns from `col` on of packed row `row`, which has adapter a >= 0.  In float32 from the float32
+// factor: the products are not the matrix instruction's.
 template <int DT>
 __device__ __forceinline__ f32x4 low_rank_of_four(const AdapterRows& ad, int row, int a, int expert, int col, int Nout) {
-  const u32x4* low = reinterpret_cast<const u32x4*>(ad.low + static_cast<int64_t>(row) * ad.rank);
+  const f32x4* wide = reinterpret_cast<const f32x4*>(ad.wide + static_cast<int64_t>(row) * ad.rank);
   const u32x4* up = reinterpret_cast<const u32x4*>(ad.up + ((static_cast<int64_t>(a) * ad.n_exp + expert) * Nout + col) * ad.rank);
   const int pieces = ad.rank >> 3;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma clang loop unroll(disable)
   for (int p = 0; p < pieces; ++p) {
-    const u32x4 l = low[p];
+    const f32x4 w[2] = {wide[2 * p], wide[2 * p + 1]};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const u32x4 u = up[i * pieces + p];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        float l0, l1, u0, u1;
-        Elem16<DT>::widen2(l[q], l0, l1);
+        float u0, u1;
         Elem16<DT>::widen2(u[q], u0, u1);
-        sum[i] = fmaf(l1, u1, fmaf(l0, u0, sum[i]));
+        sum[i] = fmaf(w[q >> 1][(q & 1) * 2 + 1], u1, fmaf(w[q >> 1][(q & 1) * 2], u0, sum[i]));
       }
     }
   }
-  return sum;
+  return ad.scale != nullptr ? sum * ad.scale[a] : sum;
 }
 
 // The kernels of 32x32x16 instructions: a k-step has two pieces, which may be two adapters' (rank 8).  acc[mi][ni] += the block of
@@ -100,16 +101,19 @@ __device__ __forceinline__ void add_low_rank32(f32x16 (&acc)[MI][NI], const Adap
         at = next_after(at);
       }
     }
-    u32x4 up[NI], low[MI];
+    u32x4 up[NI], low[2][MI];
     const bf16_t* base = ad.up + (static_cast<int64_t>(max(my_a, 0)) * ad.n_exp + expert) * Nout * ad.rank + my_p * 8;
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni)
       up[ni] = my_a >= 0 ? *reinterpret_cast<const u32x4*>(base + static_cast<int64_t>(min(col0 + ni * R + fr, Nout - 1)) * ad.rank) : zero;
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi)
-      low[mi] = my_a >= 0 && mine[mi] == my_a
-                    ? *reinterpret_cast<const u32x4*>(ad.low + static_cast<int64_t>(row0 + mi * R + fr) * ad.rank + my_p * 8)
-                    : zero;
+    for (int part = 0; part < 2; ++part)
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi)
+        low[part][mi] =
+            my_a >= 0 && mine[mi] == my_a
+                ? *reinterpret_cast<const u32x4*>(ad.low + (static_cast<int64_t>(row0 + mi * R + fr) * 2 + part) * ad.rank + my_p * 8)
+                : zero;
     uint32_t marks = 0;
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni)
@@ -133,8 +137,9 @@ __device__ __forceinline__ void add_low_rank32(f32x16 (&acc)[MI][NI], const Adap
     for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni) {
-        const vec8 u = __builtin_bit_cast(vec8, up[ni]), l = __builtin_bit_cast(vec8, low[mi]);
-        acc[mi][ni] = Elem16<DT>::mfma32(u, l, acc[mi][ni]);
+        const vec8 u = __builtin_bit_cast(vec8, up[ni]);
+        acc[mi][ni] = Elem16<DT>::mfma32(u, __builtin_bit_cast(vec8, low[0][mi]), acc[mi][ni]);
+        acc[mi][ni] = Elem16<DT>::mfma32(u, __builtin_bit_cast(vec8, low[1][mi]), acc[mi][ni]);
       }
     if (any) {
 #pragma unroll
@@ -164,7 +169,8 @@ __device__ __forceinline__ void hold(ACC& acc) {
 }
 
 // The persistent kernel's wavefront: 8 x NI blocks of 16x16x32 instructions, mine[mi] the adapter of row 16 mi + lane % 16 (-1: none,
-// or not a row of the tile), row0 and col0 its first row and column.  A step is up to 32 of one adapter's rank; blocks of 16
+// or not a row of the tile), row0 and col0 its first row and column.  A step is up to 32 of one adapter's rank, of which both summands are at hand (up to
+// rank 16 both in one operand); blocks of 16
 // rows of which none has the adapter are passed over (8192 rows of 24 requests over 8 experts: four adapters per wavefront, each
 // in a third of its rows), so a step is little work and what it costs is the latency of its operands.
 template <int DT, int NI>
@@ -178,29 +184,34 @@ __device__ __forceinline__ void add_low_rank16(f32x4 (&acc)[8][NI], const Adapte
   int lane = threadIdx.x & 63;
   asm volatile("" : "+v"(lane));   // (what follows is computed here, not kept across the K loop)
   const int fr = lane & 15, fq = lane >> 4;
-  const int pieces = ad.rank >> 3, row_bytes = ad.rank * 2;
+  const int pieces = ad.rank >> 3, row_bytes = ad.rank * 2;   // of up; twice as many of low
   constexpr uint32_t kOutside = 0x80000000u;   // no descriptor covers it: the lane gets zeros
   const __amdgpu_buffer_rsrc_t low_rsrc = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<bf16_t*>(ad.low + static_cast<int64_t>(row0) * ad.rank), 0, 0x7fffffff, 0x00020000);
+      const_cast<bf16_t*>(ad.low + static_cast<int64_t>(row0) * 2 * ad.rank), 0, 0x7fffffff, 0x00020000);
   // Half of the columns at a time: while one half's operand is multiplied the other half's, or the next step's, is on its
-  // way, and a row block's takes the next step's place as soon as both halves have used it (64 registers; more of them in flight
-  // spill, and cost more than they hide).
+  // way, and a row block's takes the next step's place as soon as both halves have used it (96 registers; the next step's in flight as well
+  // spill, and cost more than they hide).  The second summands as steps of their own, with 64: 8192 rows of 24 requests, rank 32, 2048 to 8192
+  // 340 us, 320 so, 308 with the first summands alone.
   constexpr int H = NI / 2;
-  u32x4 up[2][H], low[MI];
+  const bool split = pieces > 2;
+  u32x4 up[2][H], low[2][MI];
   auto fetch_up = [&](u32x4 (&u)[H], int first) __attribute__((always_inline)) {
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<bf16_t*>(ad.up + ((static_cast<int64_t>(at) * ad.n_exp + expert) * Nout + col0) * ad.rank), 0, 0x7fffffff, 0x00020000);
+    const int p = split || fq < pieces ? piece0 + fq : fq - pieces;
 #pragma unroll
     for (int ni = 0; ni < H; ++ni) {
-      const uint32_t off = min((first + ni) * 16 + fr, ncol - 1) * row_bytes + fq * 16;
-      u[ni] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, piece0 + fq < pieces ? off : kOutside, piece0 * 16, 0);
+      const uint32_t off = min((first + ni) * 16 + fr, ncol - 1) * row_bytes + p * 16;
+      u[ni] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, p < pieces ? off : kOutside, 0, 0);
     }
   };
   auto fetch_low = [&](int mi) __attribute__((always_inline)) {
     const bool is = mine[mi] == at;
-    if (__ballot(is) != 0)
-      low[mi] = __builtin_amdgcn_raw_buffer_load_b128(low_rsrc, is && piece0 + fq < pieces ? (mi * 16 + fr) * row_bytes + fq * 16 : kOutside,
-                                                      piece0 * 16, 0);
+    if (__ballot(is) != 0) {
+      const uint32_t off = is && piece0 + fq < (split ? pieces : 2 * pieces) ? (mi * 16 + fr) * 2 * row_bytes + fq * 16 : kOutside;
+      low[0][mi] = __builtin_amdgcn_raw_buffer_load_b128(low_rsrc, off, piece0 * 16, 0);
+      if (split) low[1][mi] = __builtin_amdgcn_raw_buffer_load_b128(low_rsrc, off, (pieces + piece0) * 16, 0);
+    }
   };
   auto clean = [&](u32x4 (&u)[H], auto first_c, int now) __attribute__((always_inline)) {
     constexpr int first = decltype(first_c)::value;
@@ -236,7 +247,12 @@ __device__ __forceinline__ void add_low_rank16(f32x4 (&acc)[8][NI], const Adapte
       if (__ballot(mine[mi] == now) != 0) {
 #pragma unroll
         for (int ni = 0; ni < H; ++ni)
-          acc[mi][first + ni] = Elem16<DT>::mfma16(__builtin_bit_cast(vec8, u[ni]), __builtin_bit_cast(vec8, low[mi]), acc[mi][first + ni]);
+          acc[mi][first + ni] = Elem16<DT>::mfma16(__builtin_bit_cast(vec8, u[ni]), __builtin_bit_cast(vec8, low[0][mi]), acc[mi][first + ni]);
+        if (split) {
+#pragma unroll
+          for (int ni = 0; ni < H; ++ni)
+            acc[mi][first + ni] = Elem16<DT>::mfma16(__builtin_bit_cast(vec8, u[ni]), __builtin_bit_cast(vec8, low[1][mi]), acc[mi][first + ni]);
+        }
       }
       if (first > 0 && more) fetch_low(mi);
     }

@@ -152,6 +152,8 @@ inline bool is_16bit(int dtype) { return dtype == MOE_BF16 || dtype == MOE_F16; 
 struct AdapterRows {
   const int32_t* of_row;
   const bf16_t* low;
+  const float* wide;            // the same in float32, without the scale if there is one
+  const float* scale;           // by adapter, or NULL
   const bf16_t* up;
   int n_exp, rank;
 };
