@@ -349,7 +349,8 @@ int moe_layer_forward_aux(const moe_config* cfg, const void* x, const void* Wg, 
  * W [n_exp, N, K], A [n_adapters, n_exp, rank, K], B [n_adapters, n_exp, N, rank], x [rows, K], y [rows, N] in dtype (BF16 or
  * F16); scale [n_adapters] float32, or NULL for ones; adapter [tokens], perm [rows], offsets [n_exp + 1] int32; v [rows, rank] float32.
  * All products are accumulated in float32 and y is rounded once.  scale v, and t of the backward, enter the second product in
- * float32 or as two summands of dtype, 16 bits with BF16 and 22 with F16 (so they have to be within an fp16 number's range with F16).  Infinities and NaNs in an adapter's A or B reach rows of
+ * float32 or as two summands of dtype, 16 bits with BF16 and 22 with F16 (of a row's largest, whatever its size up to 2^77: the summands
+ * are of the row divided by a power of two).  Infinities and NaNs in an adapter's A or B reach rows of
  * that adapter alone (B's as NaN, and up to 31 columns beside them with them); rows without an adapter have the bits they would
  * have without any.
  * rows is the most there are: rows at or beyond offsets[n_exp] are neither read nor written.

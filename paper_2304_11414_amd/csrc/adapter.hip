@@ -38,7 +38,7 @@ struct ShrinkArgs {
   const bf16_t* m;        // [n_adapters, n_exp, rank, K]
   const int32_t *offsets, *adapter, *perm;
   const float* scale;     // [n_adapters] or NULL
-  int32_t* of_row;        // out: the adapter of each packed row, or -1
+  int32_t* of_row;        // out: a word per packed row (adapter_of)
   float* wide;            // out [rows, rank]
   bf16_t* low;            // out [rows, 2 rank]: scaled, as two 16-bit summands
   int n_exp, n_adapters, top_k, K, rank, tile_rows;
@@ -50,11 +50,12 @@ struct ShrinkArgs {
 
 // (low: an operand of the matrix instruction that adds the low-rank part, as two summands, the rounding to 16 bits and that of what it
 // leaves, a row's first ones before its second ones: together 16 bits (bf16) or 22, so that the result is as good as rounded once.)
+// `power`: of two, that the row's summands are divided by.
 template <int DT>
-__device__ __forceinline__ void store_low_rank(const ShrinkArgs& a, int64_t row, int j, f32x4 v, float scale) {
+__device__ __forceinline__ void store_low_rank(const ShrinkArgs& a, int64_t row, int j, f32x4 v, float scale, int power) {
   const f32x4 scaled = v * scale;
   *reinterpret_cast<f32x4*>(a.wide + row * a.rank + j) = a.scale_wide ? scaled : v;
-  f32x4 rest = scaled;
+  f32x4 rest = DT == MOE_F16 ? scaled * two_to(-power) : scaled;
 #pragma unroll
   for (int part = 0; part < 2; ++part) {
     const u32x2 o = {Elem16<DT>::pack2(rest[0], rest[1]), Elem16<DT>::pack2(rest[2], rest[3])};
@@ -70,6 +71,19 @@ __device__ __forceinline__ void store_low_rank(const ShrinkArgs& a, int64_t row,
   }
 }
 
+__host__ __device__ inline int lanes_of_row(int rank) { return rank <= 64 ? 16 : 32; }
+
+// The bits of the largest finite magnitude of v * scale.
+__device__ __forceinline__ uint32_t largest_finite(f32x4 v, float scale) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t bits = __float_as_uint(v[e] * scale) & 0x7fffffffu;
+    top = bits < 0x7f800000u ? max(top, bits) : top;
+  }
+  return top;
+}
+
 template <int MR, int WAVES, int G>
 constexpr int kPartBytes = sizeof(float) * WAVES * 16 * G * (16 * MR + 4);
 
@@ -81,6 +95,7 @@ __global__ __launch_bounds__(64 * WAVES) void shrink_kernel(ShrinkArgs a) {
   auto part = reinterpret_cast<float(*)[16 * G][16 * MR + 4]>(shrink_lds);   // [WAVES]
   __shared__ float row_scale[16 * G];
   __shared__ int row_pair[16 * G];
+  __shared__ uint32_t row_top[DT == MOE_F16 ? 16 * G : 1];   // (fp16: of a row's factors)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 15, fq = lane >> 4;
   if (a.ticket != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
@@ -138,7 +153,8 @@ __global__ __launch_bounds__(64 * WAVES) void shrink_kernel(ShrinkArgs a) {
     if (id < 0 || id >= a.n_adapters) id = -1;
     int expert = 0;   // how many experts' rows end at or before this one
     for (int i = 1; i < a.n_exp; ++i) expert += a.offsets[i] <= row;
-    if (is && cut == 0) a.of_row[row] = id;
+    if (DT == MOE_F16) row_top[lane] = 0;
+    if (is && cut == 0 && (DT != MOE_F16 || a.cuts > 1)) a.of_row[row] = id;   // (else with its power, below)
     row_scale[lane] = id >= 0 && a.scale != nullptr ? a.scale[id] : 1.f;
     row_pair[lane] = id >= 0 && is ? id * a.n_exp + expert : -1;
   }
@@ -219,24 +235,48 @@ __global__ __launch_bounds__(64 * WAVES) void shrink_kernel(ShrinkArgs a) {
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) v += *reinterpret_cast<const f32x4*>(&part[w][q][j]);
     const int64_t row = lo + row0 + q;
-    if (a.cuts > 1) *reinterpret_cast<f32x4*>(a.partial + (cut * static_cast<int64_t>(a.rows) + row) * a.rank + j) = v;
-    else store_low_rank<DT>(a, row, j, v, row_scale[q]);
+    if (a.cuts > 1) {
+      *reinterpret_cast<f32x4*>(a.partial + (cut * static_cast<int64_t>(a.rows) + row) * a.rank + j) = v;
+    } else if (DT == MOE_F16) {
+      *reinterpret_cast<f32x4*>(&part[0][q][j]) = v;
+      atomicMax(&row_top[q], largest_finite(v, row_scale[q]));   // (the largest, in whatever order)
+    } else {
+      store_low_rank<DT>(a, row, j, v, row_scale[q], 0);
+    }
+  }
+  if (DT != MOE_F16 || a.cuts > 1) return;
+  __syncthreads();
+  for (int p = threadIdx.x; p < count * (a.rank / 4); p += 64 * WAVES) {   // (each thread what it has left there)
+    const int q = p / (a.rank / 4), j = (p - q * (a.rank / 4)) * 4;
+    const int power = power_for(row_top[q]);
+    const int64_t row = lo + row0 + q;
+    store_low_rank<DT>(a, row, j, *reinterpret_cast<const f32x4*>(&part[0][q][j]), row_scale[q], power);
+    if (j == 0) a.of_row[row] = row_word(row_pair[q] < 0 ? -1 : row_pair[q] / a.n_exp, power);
   }
 }
 
-// The shares of a cut contraction, added in order.
+// The shares of a cut contraction, added in order; 16 or 32 lanes have a row, four columns each (ranks up to 64, up to 128).
 template <int DT>
 __global__ __launch_bounds__(256) void combine_kernel(ShrinkArgs a) {
-  const int lo = a.offsets[0], quads = a.rank / 4;
-  const int64_t total = static_cast<int64_t>(a.offsets[a.n_exp] - lo) * quads;
+  const int lo = a.offsets[0], lanes = lanes_of_row(a.rank);
+  const int64_t total = static_cast<int64_t>(a.offsets[a.n_exp] - lo) * lanes;
   for (int64_t p = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; p < total; p += static_cast<int64_t>(gridDim.x) * 256) {
-    const int64_t row = lo + p / quads;
-    const int j = static_cast<int>(p % quads) * 4;
-    const int64_t at = row * a.rank + j;
+    const int64_t row = lo + p / lanes;
+    const int j = static_cast<int>(p % lanes) * 4;
+    const bool is = j < a.rank;
+    const int64_t at = row * a.rank + min(j, a.rank - 4);
     f32x4 v = *reinterpret_cast<const f32x4*>(a.partial + at);
     for (int cut = 1; cut < a.cuts; ++cut) v += *reinterpret_cast<const f32x4*>(a.partial + cut * static_cast<int64_t>(a.rows) * a.rank + at);
     const int id = a.of_row[row];
-    store_low_rank<DT>(a, row, j, v, id >= 0 && a.scale != nullptr ? a.scale[id] : 1.f);
+    const float scale = id >= 0 && a.scale != nullptr ? a.scale[id] : 1.f;
+    int power = 0;
+    if (DT == MOE_F16) {
+      uint32_t top = largest_finite(v, scale);
+      for (int off = lanes / 2; off >= 1; off >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), off, 64)));
+      power = power_for(top);
+      if (j == 0) a.of_row[row] = row_word(id, power);   // (the row's lanes, one wavefront's, have read it)
+    }
+    if (is) store_low_rank<DT>(a, row, j, v, scale, power);
   }
 }
 
@@ -318,7 +358,7 @@ __global__ __launch_bounds__(256) void count_kernel(const int32_t* __restrict__ 
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = of_row[min(r + i * 256, end - 1)];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) n += r + i * 256 < end && v[i] == id;
+      for (int i = 0; i < 4; ++i) n += r + i * 256 < end && has_adapter(v[i], id);
     }
     n = sum_of_block(n, lds);
     if (threadIdx.x == 0) {
@@ -398,7 +438,7 @@ __global__ __launch_bounds__(256) void fill_kernel(const int32_t* __restrict__ o
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = of_row[min(r + i, end - 1)];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) mine += r + i < end && v[i] == id;
+    for (int i = 0; i < 4; ++i) mine += r + i < end && has_adapter(v[i], id);
     int before = mine;   // of the wavefront's lanes up to this one
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -412,7 +452,7 @@ __global__ __launch_bounds__(256) void fill_kernel(const int32_t* __restrict__ o
     for (int w = 0; w < wave; ++w) to += lds[w];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (r + i < end && v[i] == id) g.list[to++] = r + i;
+      if (r + i < end && has_adapter(v[i], id)) g.list[to++] = r + i;
     at += lds[0] + lds[1] + lds[2] + lds[3];
   }
 }
@@ -789,7 +829,7 @@ hipError_t launch_shrink_of(const ShrinkArgs& a, int64_t rows, hipStream_t s) {
   else PPMOE_SHRINK(8, 8, 1, 2);
 #undef PPMOE_SHRINK
   if (a.cuts > 1) {
-    const int64_t blocks = (rows * (a.rank / 4) + 255) / 256;
+    const int64_t blocks = (rows * lanes_of_row(a.rank) + 255) / 256;
     combine_kernel<DT><<<static_cast<unsigned>(blocks < 4096 ? blocks : 4096), 256, 0, s>>>(a);
   }
   return hipGetLastError();

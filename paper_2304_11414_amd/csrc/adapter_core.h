@@ -28,6 +28,22 @@ struct NonFinite {   // marks (in bits 15 and 31) the elements of a word whose e
 
 constexpr int kNone = 0x7fffffff;   // after the last adapter
 
+// fp16: a row's `low` is its factor divided by a power of two, so that it is within the type's range and its small values keep their bits;
+// the row's accumulators are divided by it before the low-rank part is added and multiplied by it afterwards.  Rows whose largest factor is
+// at least 2^-4 and below 2^15 have the power 0 (the second summand is then off by 2^-21 of that factor at most), others are brought to 2^13.
+// A word of of_row: -1, or the adapter with the power in bits 16 to 23.  (bf16 has float32's range: the power is 0.)
+constexpr int kMostPower = 64, kLeastPower = -32;   // (factors up to 2^77; below 2^-19 steps of 2^-56 are finer than any result's)
+__device__ __forceinline__ int row_word(int adapter, int power) { return adapter < 0 ? -1 : adapter | (power & 0xff) << 16; }
+__device__ __forceinline__ int adapter_of(int word) { return word < 0 ? -1 : word & 0xffff; }
+__device__ __forceinline__ int power_of(int word) { return word < 0 ? 0 : static_cast<int>(static_cast<uint32_t>(word) << 8) >> 24; }
+__device__ __forceinline__ bool has_adapter(int word, int adapter) { return (word & static_cast<int>(0x8000ffffu)) == adapter; }
+__device__ __forceinline__ float two_to(int power) { return __uint_as_float(static_cast<uint32_t>(127 + power) << 23); }
+// top: the bits of the row's largest finite factor
+__device__ __forceinline__ int power_for(uint32_t top) {
+  const int e = static_cast<int>(top >> 23) - 127;
+  return top == 0 || (e >= -4 && e < 15) ? 0 : min(max(e - 13, kLeastPower), kMostPower);
+}
+
 // The least adapter above a among this lane's rows and those of the 15 lanes beside it.
 template <int MI>
 __device__ __forceinline__ int least_above(const int (&mine)[MI], int a) {
@@ -75,17 +91,29 @@ __device__ __forceinline__ void add_low_rank32(f32x16 (&acc)[MI][NI], const Adap
   const u32x4 zero = u32x4{0u, 0u, 0u, 0u};
   const int lane = threadIdx.x & 63;
   const int fr = lane & (R - 1), fq = lane / R;
-  int mine[MI];
+  int mine[MI], power[MI], any_power = 0;
 #pragma unroll
   for (int mi = 0; mi < MI; ++mi) {
     const int r = mi * R + fr;
-    mine[mi] = r < nrow ? ad.of_row[row0 + r] : -1;
+    const int word = r < nrow ? ad.of_row[row0 + r] : -1;
+    mine[mi] = adapter_of(word);
+    power[mi] = power_of(word);
+    any_power |= power[mi];
   }
+  const bool scaled = DT == MOE_F16 && __ballot(any_power != 0) != 0;
+  auto times = [&](int sign) __attribute__((always_inline)) {
+    if (!scaled) return;
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) acc[mi][ni] *= two_to(sign * power[mi]);
+  };
   auto next_after = [&](int a) __attribute__((always_inline)) -> int {
     return __builtin_amdgcn_readfirstlane(min(least_above(mine, a), __shfl_xor(least_above(mine, a), 16, 64)));
   };
   const int pieces = ad.rank >> 3;
   int at = next_after(-1), piece = 0;
+  times(-1);
 #pragma clang loop unroll(disable)
   while (at != kNone) {
     int my_a = -1, my_p = 0;   // of this lane's slot
@@ -153,9 +181,10 @@ __device__ __forceinline__ void add_low_rank32(f32x16 (&acc)[MI][NI], const Adap
           const vec8 l = __builtin_bit_cast(vec8, u32x4{w, w, w, w});
           acc[mi][ni] = Elem16<DT>::mfma32(u, l, acc[mi][ni]);
         }
-          }
+      }
     }
   }
+  times(1);
 }
 
 // Names accumulators as accumulator registers at this point of the program (left to itself the

@@ -426,7 +426,7 @@ __global__ __launch_bounds__(64 * kWaves) void data_gradient_few_rows_kernel(con
         f32x4 v = *reinterpret_cast<const f32x4*>(&part[0][m][n]);
 #pragma unroll
         for (int q = 1; q < kWaves; ++q) v += *reinterpret_cast<const f32x4*>(&part[q][m][n]);
-        const int row = lo + t0 + mt * 16 + m, id = adapters.of_row[row];
+        const int row = lo + t0 + mt * 16 + m, id = adapter_of(adapters.of_row[row]);
         if (id >= 0) v += low_rank_of_four<DT>(adapters, row, id, expert, col0 + n, Nout);
         const u32x2 o = {Elem16<DT>::pack2(v[0], v[1]), Elem16<DT>::pack2(v[2], v[3])};
         *reinterpret_cast<u32x2*>(C + static_cast<int64_t>(row) * Nout + col0 + n) = o;

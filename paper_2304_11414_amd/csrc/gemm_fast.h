@@ -552,6 +552,20 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_fast_kernel(
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   };
 
+  // Multiplies the rows of a wavefront's accumulators by their powers of two (sign 1), or divides by them (-1).
+  auto times_powers = [&](auto& acc, const int (&mine)[8], const uint32_t (&words)[8], int sign) __attribute__((always_inline)) {
+    constexpr int NI = sizeof(acc[0]) / sizeof(f32x4);
+#pragma unroll
+    for (int mi = 0; mi < 8; ++mi) {
+      const float f = two_to(mine[mi] >= 0 ? sign * power_of(static_cast<int>(words[mi])) : 0);
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) {
+        acc[mi][ni] *= f;
+        asm volatile("" : "+a"(acc[mi][ni]));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
   // ADAPT: adds the rows' adapters to a tile's accumulators, of this wavefront the rows from row_base and columns from col_base on.
   auto add_adapters = [&](auto& acc, const Segment& s, int row_base, int col_base) __attribute__((always_inline)) {
     constexpr int NI = sizeof(acc[0]) / sizeof(f32x4);
@@ -563,8 +577,24 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_fast_kernel(
     for (int mi = 0; mi < 8; ++mi) v[mi] = row_base + mi * 16 + fr_l;
     lds_read_words(v, lds_address(row_list) + s.list * (BM * 4));
 #pragma unroll
-    for (int mi = 0; mi < 8; ++mi) mine[mi] = row_base + mi * 16 + fr_l < s.rows ? static_cast<int>(v[mi]) : -1;
+    for (int mi = 0; mi < 8; ++mi) mine[mi] = row_base + mi * 16 + fr_l < s.rows ? adapter_of(static_cast<int>(v[mi])) : -1;
+    bool scaled = false;
+    if constexpr (DT == MOE_F16) {
+      int any = 0;
+#pragma unroll
+      for (int mi = 0; mi < 8; ++mi) any |= mine[mi] >= 0 ? power_of(static_cast<int>(v[mi])) : 0;
+      scaled = __ballot(any != 0) != 0;
+      if (scaled) times_powers(acc, mine, v, -1);
+    }
     add_low_rank16<DT, NI>(acc, adapters, mine, s.expert, s.row0 + row_base, s.col0 + col_base, Nout);
+    if constexpr (DT == MOE_F16) {
+      if (scaled) {   // (the words are read again: kept, they would cost registers in between)
+#pragma unroll
+        for (int mi = 0; mi < 8; ++mi) v[mi] = row_base + mi * 16 + fr_l;
+        lds_read_words(v, lds_address(row_list) + s.list * (BM * 4));
+        times_powers(acc, mine, v, 1);
+      }
+    }
   };
 
   Segment nxt = next_segment(), pending = {};

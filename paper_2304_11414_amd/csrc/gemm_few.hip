@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kThreads, 4) void grouped_gemm_few_rows_kernel(
   // Finishes four columns of packed row `row`.
   auto store = [&](int row, int n, f32x4 v) __attribute__((always_inline)) {
     if constexpr (ADAPT) {
-      const int a = adapters.of_row[row];
+      const int a = adapter_of(adapters.of_row[row]);
       if (a >= 0) v += low_rank_of_four<DT>(adapters, row, a, expert, col0 + n, Nout);
     }
     if (GELU) v = gelu_tanh4(v);

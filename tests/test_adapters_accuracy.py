@@ -68,3 +68,27 @@ TILES = [((130, 7), 72, 136, 3, 8, dict()), ((300, 500), 328, 1000, 4, 40, dict(
 @pytest.mark.parametrize("shape", TILES, ids=[str(i) for i in range(len(TILES))])
 def test_tiles(shape, dt):
     check_both(shape, dt)
+
+
+@pytest.mark.parametrize("projection", [True, False], ids=["projection", "zeros"])
+@pytest.mark.parametrize("shape", FEW + TILES, ids=[str(i) for i in range(len(FEW + TILES))])
+def test_fp16_factors_of_any_size(shape, projection):
+    """scale v and t far beyond fp16's range, and far below it, where y and dx are not: rows of adapters of several sizes side by side."""
+    counts, K, N, n_a, rank, more = shape
+    sizes = [2.0 ** (18, 0, -20, 10, -12, 30)[i % 6] for i in range(n_a)]
+    back = [2.0 ** (-10, 0, 10, -6, 8, -14)[i % 6] for i in range(n_a)]
+    for backward in (False, True):
+        c = Case(counts, K, N, n_a, rank, "f16", seed=K + rank + 1, **{**more, "gelu": False})
+        c.scale = torch.tensor(sizes, device="cuda")
+        second = c.A if backward else c.B
+        second.mul_(torch.tensor(back, device="cuda", dtype=torch.float16).view(-1, 1, 1, 1))
+        if sizes[-1] == 2.0 ** 30 or n_a > 5:      # 2^30 * 2^-14 * 2^-14 in the other factor as well
+            (c.B if backward else c.A)[5::6].mul_(2.0 ** -8)
+        if not projection:
+            c.W.zero_()
+        x, dy, W, A, Bm = (f64(t) for t in (c.x, c.dy, c.W, c.A, c.B))
+        if not backward:
+            check_product(c, f64(c.forward()[0]), x, W, A, Bm)
+        else:
+            v = torch.zeros(c.rows + 5, rank, device="cuda")
+            check_product(c, f64(c.backward(v)[0]), dy, W.transpose(0, 2, 1), Bm.transpose(0, 1, 3, 2), A.transpose(0, 1, 3, 2))
