@@ -351,8 +351,8 @@ int moe_layer_forward_aux(const moe_config* cfg, const void* x, const void* Wg, 
  * All products are accumulated in float32 and y is rounded once.  scale v, and t of the backward, enter the second product in
  * float32 or as two summands of dtype, 16 bits with BF16 and 22 with F16 (of a row's largest, whatever its size up to 2^77: the summands
  * are of the row divided by a power of two).  Infinities and NaNs in an adapter's A or B reach rows of
- * that adapter alone (B's as NaN, and up to 31 columns beside them with them); rows without an adapter have the bits they would
- * have without any.
+ * that adapter alone, those of B (in dx: of A) their own column of these rows alone, as NaN or infinite; rows without an adapter have the
+ * bits they would have without any.
  * rows is the most there are: rows at or beyond offsets[n_exp] are neither read nor written.
  * Limits: rows >= 0, K and N multiples of 8 up to 2^20, n_exp <= 256, n_exp * n_adapters <= 65536, rank a multiple of 8 up to 128,
  * top_k <= 8.

@@ -10,7 +10,7 @@
 // contraction of 1024.
 //
 // 0 * infinity would carry an adapter's infinities and NaNs to other requests' rows.  They are looked for in the operand,
-// replaced by zeros where there are any, and the blocks of columns they are in become NaN in that adapter's own rows.
+// replaced by zeros where there are any, and their columns become infinite in that adapter's own rows.
 #pragma once
 
 #include <type_traits>
@@ -25,6 +25,13 @@ struct NonFinite {   // marks (in bits 15 and 31) the elements of a word whose e
   static __device__ __forceinline__ uint32_t marks(uint32_t w) { return ((w & kExponent) + kOne) & 0x80008000u; }
   static __device__ __forceinline__ uint32_t cleared(uint32_t w) { return w & ~((marks(w) >> 15) * 0xffffu); }
 };
+
+// An operand (of a bf16 product, whatever the other types) of the largest numbers, or of zeros: a product of two such is infinite
+// where both have the numbers, and nothing elsewhere.
+__device__ __forceinline__ bf16x8 overflowing(bool is) {
+  const uint32_t w = is ? 0x7f7f7f7fu : 0u;
+  return __builtin_bit_cast(bf16x8, u32x4{w, w, w, w});
+}
 
 constexpr int kNone = 0x7fffffff;   // after the last adapter
 
@@ -173,14 +180,10 @@ __device__ __forceinline__ void add_low_rank32(f32x16 (&acc)[MI][NI], const Adap
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni) {
         if (bad[ni] == 0) continue;
-        const bool slot = ((bad[ni] >> (fq * R)) & ((uint64_t(1) << R) - 1)) != 0;
-        const vec8 u = __builtin_bit_cast(vec8, up[ni]);
+        const bf16x8 u = overflowing((bad[ni] >> lane) & 1);
 #pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
-          const uint32_t w = slot && my_a >= 0 && mine[mi] == my_a ? 0x7fff7fffu : 0u;
-          const vec8 l = __builtin_bit_cast(vec8, u32x4{w, w, w, w});
-          acc[mi][ni] = Elem16<DT>::mfma32(u, l, acc[mi][ni]);
-        }
+        for (int mi = 0; mi < MI; ++mi)
+          acc[mi][ni] = Elem16<MOE_BF16>::mfma32(u, overflowing(my_a >= 0 && mine[mi] == my_a), acc[mi][ni]);
       }
     }
   }
@@ -259,11 +262,10 @@ __device__ __forceinline__ void add_low_rank16(f32x4 (&acc)[8][NI], const Adapte
         u[ni][q] = NonFinite<DT>::cleared(u[ni][q]);
       }
       if (__ballot(m != 0) != 0) {
+        const bf16x8 column = overflowing(m != 0);
 #pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
-          const uint32_t w = mine[mi] == now ? 0x7fff7fffu : 0u;
-          acc[mi][first + ni] = Elem16<DT>::mfma16(__builtin_bit_cast(vec8, u[ni]), __builtin_bit_cast(vec8, u32x4{w, w, w, w}), acc[mi][first + ni]);
-        }
+        for (int mi = 0; mi < MI; ++mi)
+          acc[mi][first + ni] = Elem16<MOE_BF16>::mfma16(column, overflowing(mine[mi] == now), acc[mi][first + ni]);
       }
     }
     hold<MI, NI>(acc);
