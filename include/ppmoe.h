@@ -347,7 +347,8 @@ int moe_layer_forward_aux(const moe_config* cfg, const void* x, const void* Wg, 
  *   u[r, :] = W[i] x[r, :] + scale[a] B[a][i] v[r, :]                   [N]
  *   y[r, :] = u[r, :], or GeLU(u[r, :]) (tanh form) with MOE_ACT_GELU
  * W [n_exp, N, K], A [n_adapters, n_exp, rank, K], B [n_adapters, n_exp, N, rank], x [rows, K], y [rows, N] in dtype (BF16 or
- * F16); scale [n_adapters] float32, or NULL for ones; adapter [tokens], perm [rows], offsets [n_exp + 1] int32; v [rows, rank] float32.
+ * F16); scale [n_adapters] float32, or NULL for ones; adapter [tokens] ([rows] when perm is NULL), perm [rows], offsets [n_exp + 1]
+ * int32; v [rows, rank] float32.
  * All products are accumulated in float32 and y is rounded once.  scale v, and t of the backward, enter the second product in
  * float32 or as two summands of dtype, 16 bits with BF16 and 22 with F16 (of a row's largest, whatever its size up to 2^77: the summands
  * are of the row divided by a power of two).  Infinities and NaNs in an adapter's A or B reach rows of
@@ -366,7 +367,7 @@ int moe_layer_forward_aux(const moe_config* cfg, const void* x, const void* Wg, 
  * Sums have a fixed order: the same bits on every run.  Neither call allocates or, after moe_init, synchronises.
  * workspace: at least moe_adapter_workspace_bytes / moe_adapter_backward_workspace_bytes bytes (0 on an invalid config); calls
  * that share one must be ordered on one stream.  An output or the workspace that overlaps any other array of the call is refused
- * (MOE_ERR_OVERLAP): neither call works in place. */
+ * (MOE_ERR_OVERLAP; of `adapter` with perm the first element counts, as its size is not known): neither call works in place. */
 enum { MOE_ACT_NONE = 0, MOE_ACT_GELU = 1 };
 typedef struct {
   int32_t rows, K, N;

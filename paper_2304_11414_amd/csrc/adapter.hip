@@ -800,6 +800,11 @@ bool overlapping(const Memory (&m)[N], int written) {
   return false;
 }
 
+// What the call knows of the size of `adapter`: a token per row without perm, else at least one.
+size_t bytes_of_adapter(const moe_adapter_config& c, const int32_t* perm) {
+  return c.rows == 0 ? 0 : perm == nullptr ? static_cast<size_t>(c.rows) * 4 : 4;
+}
+
 template <int DT>
 hipError_t launch_shrink_of(const ShrinkArgs& a, int64_t rows, hipStream_t s) {
   const int64_t tiles = (rows + a.tile_rows - 1) / a.tile_rows * a.cuts;
@@ -888,7 +893,7 @@ int moe_adapter_forward(const moe_adapter_config* cfg, const void* x, const int3
   const size_t n_rows = cfg->rows, pairs = static_cast<size_t>(cfg->n_exp) * cfg->n_adapters, k = cfg->K, n = cfg->N, r = cfg->rank;
   const adapter::Memory memory[] = {{y, n_rows * n * 2}, {v, n_rows * r * 4}, {workspace, L.total}, {x, n_rows * k * 2},
                                     {offsets, (cfg->n_exp + 1) * size_t(4)}, {W, cfg->n_exp * n * k * 2}, {A, pairs * r * k * 2},
-                                    {B, pairs * n * r * 2}, {scale, cfg->n_adapters * size_t(4)}, {adapter, 4}, {perm, n_rows * 4}};
+                                    {B, pairs * n * r * 2}, {scale, cfg->n_adapters * size_t(4)}, {adapter, adapter::bytes_of_adapter(*cfg, perm)}, {perm, n_rows * 4}};
   if (adapter::overlapping(memory, 3)) return MOE_ERR_OVERLAP;
   hipStream_t s = static_cast<hipStream_t>(stream);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
@@ -926,7 +931,7 @@ int moe_adapter_backward(const moe_adapter_config* cfg, const void* x, const int
     const size_t n_rows = cfg->rows, k = K, n = N, a = pairs * rank * k, b = pairs * rank * n;
     const adapter::Memory memory[] = {{dx, n_rows * k * 2}, {dA, a * 4}, {dB, b * 4}, {workspace, L.total}, {x, n_rows * k * 2},
                                       {offsets, (n_exp + 1) * size_t(4)}, {W, n_exp * n * k * 2}, {A, a * 2}, {B, b * 2},
-                                      {scale, cfg->n_adapters * size_t(4)}, {adapter, n_rows > 0 ? 4u : 0u}, {perm, n_rows * 4},
+                                      {scale, cfg->n_adapters * size_t(4)}, {adapter, adapter::bytes_of_adapter(*cfg, perm)}, {perm, n_rows * 4},
                                       {dy, n_rows * n * 2}, {v, n_rows * rank * 4}};
     if (adapter::overlapping(memory, 4)) return MOE_ERR_OVERLAP;
   }
