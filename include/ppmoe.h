@@ -355,7 +355,7 @@ int moe_layer_forward_aux(const moe_config* cfg, const void* x, const void* Wg, 
  * that adapter alone, those of B (in dx: of A) their own column of these rows alone, as NaN or infinite; rows without an adapter have the
  * bits they would have without any.
  * rows is the most there are: rows at or beyond offsets[n_exp] are neither read nor written.
- * Limits: rows >= 0, K and N multiples of 8 up to 2^20, n_exp <= 256, n_exp * n_adapters <= 65536, rank a multiple of 8 up to 128,
+ * Limits: 0 <= rows <= 2^28 - 256, K and N multiples of 8 up to 2^20, n_exp <= 256, n_exp * n_adapters <= 65536, rank a multiple of 8 up to 128,
  * top_k <= 8.
  * moe_adapter_backward, from dy = dLoss/du (activation MOE_ACT_NONE only) and the v the forward left:
  *   t[r, :]  = scale[a] B[a][i]^T dy[r, :]

@@ -20,6 +20,7 @@ namespace adapter {
 constexpr int kMaxRank = 128;
 constexpr int kMaxPairs = 1 << 16;   // adapters x experts
 constexpr int kMaxColumns = 1 << 20;
+constexpr int kMaxRows = (1 << 28) - 256;   // 32 rows a block of 512 threads: below the 2^32 threads that a launch may have
 
 // ---- x A^T: [rows, K] with a matrix [rank, K] of each row's own ------------------------------------------
 //
@@ -697,7 +698,7 @@ inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) &
 
 int check_config(const moe_adapter_config* c) {
   if (c == nullptr) return MOE_ERR_NULL;
-  if (c->rows < 0 || c->K <= 0 || c->N <= 0 || (c->K & 7) || (c->N & 7) || c->K > kMaxColumns || c->N > kMaxColumns) return MOE_ERR_SHAPE;
+  if (c->rows < 0 || c->rows > kMaxRows || c->K <= 0 || c->N <= 0 || (c->K & 7) || (c->N & 7) || c->K > kMaxColumns || c->N > kMaxColumns) return MOE_ERR_SHAPE;
   if (c->n_exp < 1 || c->n_exp > kMaxExperts || c->n_adapters < 1 || c->n_adapters > kMaxPairs / c->n_exp) return MOE_ERR_SHAPE;
   if (c->rank < 8 || c->rank > kMaxRank || (c->rank & 7) || c->top_k < 1 || c->top_k > kMaxTopK) return MOE_ERR_SHAPE;
   if (!is_16bit(c->dtype)) return MOE_ERR_DTYPE;
@@ -710,7 +711,8 @@ int check_config(const moe_adapter_config* c) {
 // the backward of 4096 rows of 2048 from 8192, rank 64: 224 and 218 us; of 1024 from 1024, 8 adapters: 61 and 58.
 int rows_of_piece(const moe_adapter_config& c, int C) {
   const int64_t col_blocks = (C + kGradColumns - 1) / kGradColumns;
-  const int64_t n = (c.rows * col_blocks + 255) / 256;
+  int64_t n = (c.rows * col_blocks + 255) / 256;
+  if (n > c.rows) n = c.rows;   // (more than 256 blocks side by side already)
   return static_cast<int>(n < 256 ? 256 : (n + kGradRows - 1) / kGradRows * kGradRows);
 }
 int64_t most_pieces(const moe_adapter_config& c, int C) {
