@@ -507,7 +507,10 @@ __device__ __forceinline__ void gradient_piece(const BothGrads& b, const GradArg
       const int q = p / quads;
       const f32x4 v = *reinterpret_cast<const f32x4*>(a.u + static_cast<int64_t>(list[q]) * rank + (p - q * quads) * 4);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(v[e] * s));
+      for (int e = 0; e < 4; ++e) {
+        const float m = fabsf(v[e] * s);
+        top = m < __builtin_inff() ? fmaxf(top, m) : top;   // (infinities and NaNs stay what they are at any scale)
+      }
     }
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
@@ -515,7 +518,7 @@ __device__ __forceinline__ void gradient_piece(const BothGrads& b, const GradArg
     __syncthreads();
     top = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
     const int e = static_cast<int>(__float_as_uint(top) >> 23) - 127;
-    if (e > -110 && e < 128) {   // (zeros, and what is beyond any use, as they are; infinities too)
+    if (e > -110) {   // (zeros, and what is beyond any use, as they are)
       up = __uint_as_float(static_cast<uint32_t>(127 + 13 - e) << 23);
       down = __uint_as_float(static_cast<uint32_t>(127 - 13 + e) << 23);
     }
