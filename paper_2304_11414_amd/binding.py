@@ -362,11 +362,41 @@ def moe_adapter_workspace_bytes(cfg) -> int:
     return load_library().moe_adapter_workspace_bytes(byref(cfg))
 
 
+def _addresses(what, stream, arrays):
+    """The addresses of (name, tensor or None, dtype or None, least number of elements).  Refuses what the kernels would misread: every tensor
+    has to be contiguous on the current device, whose stream the call takes.  (4 us of host time for an adapter call.)"""
+    import torch
+    device, at = torch.cuda.current_device(), []
+    for name, t, dtype, least in arrays:
+        if t is None:
+            at.append(None)
+            continue
+        if t.get_device() != device or (t.dtype is not dtype and dtype is not None) or t.numel() < least or not t.is_contiguous():
+            raise MoeError(f"{what}: {name} must be a contiguous tensor of {dtype or 'any type'} on the current device, {least} elements or more")
+        at.append(t.data_ptr())
+    if stream is not None and getattr(stream, "device_index", device) != device:
+        raise MoeError(f"{what}: the stream is not one of the current device")
+    return at
+
+
+def _adapter_arrays(cfg, x, offsets, W, A, B, scale, adapter, perm):
+    """Those that both directions read, their common type, and the sizes of [rows, K], [rows, N], [rows, rank], A and B."""
+    import torch
+    rows, K, N, n_exp, n_adapters, rank = cfg.rows, cfg.K, cfg.N, cfg.n_exp, cfg.n_adapters, cfg.rank
+    half = torch.float16 if cfg.dtype == MOE_F16 else torch.bfloat16
+    pairs = n_exp * n_adapters
+    size_x, size_a, size_b = rows * K, pairs * rank * K, pairs * N * rank
+    return [("x", x, half, size_x), ("offsets", offsets, torch.int32, n_exp + 1), ("W", W, half, n_exp * N * K), ("A", A, half, size_a),
+            ("B", B, half, size_b), ("scale", scale, torch.float32, n_adapters), ("adapter", adapter, torch.int32, 1 if rows > 0 else 0),
+            ("perm", perm, torch.int32, rows)], half, size_x, rows * N, rows * rank, size_a, size_b
+
+
 def moe_adapter_forward(cfg, x, offsets, W, A, B, scale, adapter, perm, y, v, workspace, stream=None):
     """The grouped projection with each row's adapter beside it (scale and perm may be None)."""
-    _check(load_library().moe_adapter_forward(
-        byref(cfg), _ptr(x), _ptr(offsets), _ptr(W), _ptr(A), _ptr(B), _ptr(scale), _ptr(adapter), _ptr(perm), _ptr(y), _ptr(v),
-        _ptr(workspace), _nbytes(workspace), _stream(stream)), "moe_adapter_forward")
+    import torch
+    arrays, half, _, size_y, size_v, _, _ = _adapter_arrays(cfg, x, offsets, W, A, B, scale, adapter, perm)
+    at = _addresses("moe_adapter_forward", stream, arrays + [("y", y, half, size_y), ("v", v, torch.float32, size_v), ("workspace", workspace, None, 0)])
+    _check(load_library().moe_adapter_forward(byref(cfg), *at, _nbytes(workspace), _stream(stream)), "moe_adapter_forward")
 
 
 def moe_adapter_backward_workspace_bytes(cfg) -> int:
@@ -375,9 +405,13 @@ def moe_adapter_backward_workspace_bytes(cfg) -> int:
 
 def moe_adapter_backward(cfg, x, offsets, W, A, B, scale, adapter, perm, dy, v, dx, dA, dB, workspace, stream=None):
     """Its gradients with W frozen (scale, perm and dx may be None); dA and dB are float32 and overwritten."""
-    _check(load_library().moe_adapter_backward(
-        byref(cfg), _ptr(x), _ptr(offsets), _ptr(W), _ptr(A), _ptr(B), _ptr(scale), _ptr(adapter), _ptr(perm), _ptr(dy), _ptr(v),
-        _ptr(dx), _ptr(dA), _ptr(dB), _ptr(workspace), _nbytes(workspace), _stream(stream)), "moe_adapter_backward")
+    import torch
+    f32 = torch.float32
+    arrays, half, size_x, size_y, size_v, size_a, size_b = _adapter_arrays(cfg, x, offsets, W, A, B, scale, adapter, perm)
+    at = _addresses("moe_adapter_backward", stream, arrays + [
+        ("dy", dy, half, size_y), ("v", v, f32, size_v), ("dx", dx, half, size_x), ("dA", dA, f32, size_a), ("dB", dB, f32, size_b),
+        ("workspace", workspace, None, 0)])
+    _check(load_library().moe_adapter_backward(byref(cfg), *at, _nbytes(workspace), _stream(stream)), "moe_adapter_backward")
 
 
 def make_adamw_config(beta1=0.9, beta2=0.999, eps=1e-8, moment_bits=32) -> MoeAdamwConfig:
@@ -429,18 +463,21 @@ def moe_adamw_plan(cfg, tensors) -> AdamwPlan:
     return AdamwPlan(host.to(device or "cuda"), len(tensors), chunks.value, list(tensors))
 
 
-def moe_adamw_scalars(step, lr, grad_scale=1.0, skip=False, out=None):
-    """The values of a step in device memory (int32 step and skip, float32 lr and grad_scale); `out`: such a tensor, overwritten."""
+def moe_adamw_scalars(step, lr, grad_scale=1.0, skip=False, out=None, device=None):
+    """The values of a step in device memory (int32 step and skip, float32 lr and grad_scale) of `device` (the current one); `out`:
+    such a tensor, overwritten."""
     import torch
     host = torch.empty(4, dtype=torch.int32)
     host[0], host[1] = int(step), int(bool(skip))
     host[2:].view(torch.float32).copy_(torch.tensor([lr, grad_scale], dtype=torch.float32))
-    return host.cuda() if out is None else out.copy_(host)
+    return host.to("cuda" if device is None else device) if out is None else out.copy_(host)
 
 
 def moe_adamw_step(cfg, plan, values, stream=None):
-    _check(load_library().moe_adamw_step(byref(cfg), _ptr(plan.memory), plan.n_tensors, plan.n_chunks, _ptr(values),
-                                         _stream(stream)), "moe_adamw_step")
+    """One step over the plan's tensors with moe_adamw_scalars' values, on the plan's device, which has to be the current one."""
+    import torch
+    at, values_at = _addresses("moe_adamw_step", stream, [("the plan", plan.memory, torch.uint8, 0), ("values", values, torch.int32, 4)])
+    _check(load_library().moe_adamw_step(byref(cfg), at, plan.n_tensors, plan.n_chunks, values_at, _stream(stream)), "moe_adamw_step")
 
 
 def moe_copy_bytes(src, dst, stream=None):
