@@ -112,27 +112,25 @@ __global__ __launch_bounds__(64 * WAVES) void shrink_kernel(ShrinkArgs a) {
   const int k_end = min(a.K, (cut + 1) * stretches / a.cuts * kStretch), k_begin = cut * stretches / a.cuts * kStretch;
   // Two k-steps of 16 rows are fetched as eight rows of 128 bytes each, whole lines (rows may be a power of two apart, and then one line of each
   // of 16 rows is more than their set of the cache holds until its other half is asked for), and change places in LDS of the
-  // wavefront's own.  One k-step (J 1) comes as the operand is.
-  constexpr bool kLines = J % 2 == 0;
+  // wavefront's own.
+  static_assert(J % 2 == 0, "k-steps come in pairs");
   unsigned char* own = reinterpret_cast<unsigned char*>(shrink_lds) + kPartBytes<MR, WAVES, G> + wave * 2048;
-  auto row_at = [&](int j) __attribute__((always_inline)) -> int { return kLines ? (j & 1) * 8 + (lane >> 3) : fr; };   // of 16
-  auto k_at = [&](int j) __attribute__((always_inline)) -> int { return kLines ? (j >> 1) * 64 + (lane & 7) * 8 : 32 * j + fq * 8; };
+  auto row_at = [&](int j) __attribute__((always_inline)) -> int { return (j & 1) * 8 + (lane >> 3); };   // of 16
+  auto k_at = [&](int j) __attribute__((always_inline)) -> int { return (j >> 1) * 64 + (lane & 7) * 8; };
   auto settle = [&](auto& v) __attribute__((always_inline)) {
-    if constexpr (kLines) {
-      constexpr int N = sizeof(v[0]) / sizeof(u32x4);
+    constexpr int N = sizeof(v[0]) / sizeof(u32x4);
 #pragma unroll
-      for (int j = 0; j < J; j += 2)
+    for (int j = 0; j < J; j += 2)
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
+      for (int n = 0; n < N; ++n) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int row = row_at(h);
-            *reinterpret_cast<u32x4*>(own + row * 128 + (((lane & 7) ^ (row & 7)) << 4)) = v[j + h][n];
-          }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) v[j + h][n] = *reinterpret_cast<const u32x4*>(own + fr * 128 + (((h * 4 + fq) ^ (fr & 7)) << 4));
+        for (int h = 0; h < 2; ++h) {
+          const int row = row_at(h);
+          *reinterpret_cast<u32x4*>(own + row * 128 + (((lane & 7) ^ (row & 7)) << 4)) = v[j + h][n];
         }
-    }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) v[j + h][n] = *reinterpret_cast<const u32x4*>(own + fr * 128 + (((h * 4 + fq) ^ (fr & 7)) << 4));
+      }
   };
   const u32x4 zero = u32x4{0u, 0u, 0u, 0u};
   u32x4 x[J][G];
