@@ -36,8 +36,10 @@ __device__ __forceinline__ bf16x8 overflowing(bool is) {
 constexpr int kNone = 0x7fffffff;   // after the last adapter
 
 // fp16: a row's `low` is its factor divided by a power of two, so that it is within the type's range and its small values keep their bits;
-// the row's accumulators are divided by it before the low-rank part is added and multiplied by it afterwards.  Rows whose largest factor is
-// at least 2^-4 and below 2^15 have the power 0 (the second summand is then off by 2^-21 of that factor at most), others are brought to 2^13.
+// the row's accumulators are divided by it before the low-rank part is added and multiplied by it afterwards (add_low_rank32; the persistent
+// kernel, whose accumulators take all registers, adds such rows in its epilogue, in float32 as the kernels of few rows do).  Rows whose largest
+// factor is at least 2^-4 and below 2^15 have the power 0 (the second summand is then off by 2^-21 of that factor at most), others are
+// brought to 2^13.
 // A word of of_row: -1, or the adapter with the power in bits 16 to 23.  (bf16 has float32's range: the power is 0.)
 constexpr int kMostPower = 64, kLeastPower = -32;   // (factors up to 2^77; below 2^-19 steps of 2^-56 are finer than any result's)
 __device__ __forceinline__ int row_word(int adapter, int power) { return adapter < 0 ? -1 : adapter | (power & 0xff) << 16; }
@@ -252,7 +254,7 @@ __device__ __forceinline__ void add_low_rank16(f32x4 (&acc)[8][NI], const Adapte
     for (int ni = 0; ni < H; ++ni)
 #pragma unroll
       for (int q = 0; q < 4; ++q) marks |= NonFinite<DT>::marks(u[ni][q]);
-    if (__ballot(marks != 0) == 0) return;
+    if (__builtin_expect(__ballot(marks != 0) == 0, 1)) return;
 #pragma unroll
     for (int ni = 0; ni < H; ++ni) {
       uint32_t m = 0;

@@ -552,49 +552,29 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_fast_kernel(
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   };
 
-  // Multiplies the rows of a wavefront's accumulators by their powers of two (sign 1), or divides by them (-1).
-  auto times_powers = [&](auto& acc, const int (&mine)[8], const uint32_t (&words)[8], int sign) __attribute__((always_inline)) {
-    constexpr int NI = sizeof(acc[0]) / sizeof(f32x4);
-#pragma unroll
-    for (int mi = 0; mi < 8; ++mi) {
-      const float f = two_to(mine[mi] >= 0 ? sign * power_of(static_cast<int>(words[mi])) : 0);
-#pragma unroll
-      for (int ni = 0; ni < NI; ++ni) {
-        acc[mi][ni] *= f;
-        asm volatile("" : "+a"(acc[mi][ni]));
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
   // ADAPT: adds the rows' adapters to a tile's accumulators, of this wavefront the rows from row_base and columns from col_base on.
-  auto add_adapters = [&](auto& acc, const Segment& s, int row_base, int col_base) __attribute__((always_inline)) {
+  // Returns which of this lane's rows are left to the epilogue, a bit for each block of 16 (fp16: those whose word has a power of two, in
+  // float32 there: multiplying the accumulators around the sum spills some of them, 4 us of a launch of one tile per CU whether there are
+  // such rows or not).
+  auto add_adapters = [&](auto& acc, const Segment& s, int row_base, int col_base) __attribute__((always_inline)) -> int {
     constexpr int NI = sizeof(acc[0]) / sizeof(f32x4);
     int fr_l = lane & 15;
     asm volatile("" : "+v"(fr_l));
     uint32_t v[8];
-    int mine[8];
+    int mine[8], left = 0;
 #pragma unroll
     for (int mi = 0; mi < 8; ++mi) v[mi] = row_base + mi * 16 + fr_l;
     lds_read_words(v, lds_address(row_list) + s.list * (BM * 4));
 #pragma unroll
-    for (int mi = 0; mi < 8; ++mi) mine[mi] = row_base + mi * 16 + fr_l < s.rows ? adapter_of(static_cast<int>(v[mi])) : -1;
-    bool scaled = false;
-    if constexpr (DT == MOE_F16) {
-      int any = 0;
-#pragma unroll
-      for (int mi = 0; mi < 8; ++mi) any |= mine[mi] >= 0 ? power_of(static_cast<int>(v[mi])) : 0;
-      scaled = __ballot(any != 0) != 0;
-      if (scaled) times_powers(acc, mine, v, -1);
-    }
-    add_low_rank16<DT, NI>(acc, adapters, mine, s.expert, s.row0 + row_base, s.col0 + col_base, Nout);
-    if constexpr (DT == MOE_F16) {
-      if (scaled) {   // (the words are read again: kept, they would cost registers in between)
-#pragma unroll
-        for (int mi = 0; mi < 8; ++mi) v[mi] = row_base + mi * 16 + fr_l;
-        lds_read_words(v, lds_address(row_list) + s.list * (BM * 4));
-        times_powers(acc, mine, v, 1);
+    for (int mi = 0; mi < 8; ++mi) {
+      mine[mi] = row_base + mi * 16 + fr_l < s.rows ? static_cast<int>(v[mi]) : -1;
+      if (DT == MOE_F16 && mine[mi] > 0xffff) {
+        mine[mi] = -1;
+        left |= 1 << mi;
       }
     }
+    add_low_rank16<DT, NI>(acc, adapters, mine, s.expert, s.row0 + row_base, s.col0 + col_base, Nout);
+    return left;
   };
 
   Segment nxt = next_segment(), pending = {};
@@ -628,7 +608,7 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_fast_kernel(
     const int tiles = cur.ke - cur.kb;
     // What follows a segment's K loop: who writes the tile, the next segment's loads, the epilogue.  (One copy for big
     // tiles and one for small ones: accumulators that both kinds of K loop feed cost the compiler copies inside the loops.)
-    auto finish_segment = [&](auto& acc, auto ni_c) __attribute__((always_inline)) {
+    auto finish_segment = [&](auto& acc, auto ni_c, int rows_left) __attribute__((always_inline)) {
     constexpr int NI = decltype(ni_c)::value;   // 16-column blocks of a wavefront
     __builtin_amdgcn_s_barrier();   // every wavefront is done with the ring
 
@@ -814,7 +794,8 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_fast_kernel(
             for (int ni = 0; ni < NI; ++ni) v[ni] += p[j][ni];
         }
       };
-      const bool plain = full && mode == 0 && n_contrib == 0;
+      const bool any_left = ADAPT && DT == MOE_F16 && __ballot(rows_left != 0) != 0;
+      const bool plain = full && mode == 0 && n_contrib == 0 && !any_left;
       if (plain) {
         if constexpr (NI == 8) {
         // (no branches: they cost a wavefront that is alone on its SIMD more than the work they would skip)
@@ -873,6 +854,17 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_fast_kernel(
             case 5: fetch(IC<5>{}); break;
             case 6: fetch(IC<6>{}); break;
             default: fetch(IC<7>{}); break;
+          }
+          if constexpr (ADAPT && DT == MOE_F16) {
+            // (the words from memory: the list in LDS may be the next segment's already)
+            if (__builtin_expect(any_left, 0) && ((rows_left >> mi) & 1)) {
+              const int row = cur.row0 + row_base + mi * 16 + fr_l, a = adapter_of(adapters.of_row[row]);
+#pragma unroll
+              for (int ni = 0; ni < NI; ++ni) {
+                const int col = cur.col0 + col_base + ni * 16 + fq_l * 4;
+                if (col < Nout) v[ni] += low_rank_of_four<DT>(adapters, row, a, cur.expert, col, Nout);
+              }
+            }
           }
           // Partial sums are added in CU order (fixed summation order); the loads of several CUs' slots go out
           // together, so that the wait is one memory latency for them all.
@@ -950,9 +942,10 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_fast_kernel(
 #pragma unroll
         for (int ni = 0; ni < 8; ++ni) acc[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
       k_loop<DT, false, B_BY_ROWS, kStores>(acc, a_base, b_base, tiles, stores_behind, load_big);
+      int rows_left = 0;
       if constexpr (ADAPT)
-        if (cur.kb == 0) add_adapters(acc, cur, wm * 128, wn * 128);
-      finish_segment(acc, IC<8>{});
+        if (cur.kb == 0) rows_left = add_adapters(acc, cur, wm * 128, wn * 128);
+      finish_segment(acc, IC<8>{}, rows_left);
     } else {
       f32x4 acc[8][4];
 #pragma unroll
@@ -962,9 +955,10 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_fast_kernel(
       if (cur.kind == 1) small_loop(IC<1>{}, acc, tiles, stores_behind);
       else if (cur.kind == 2) small_loop(IC<2>{}, acc, tiles, stores_behind);
       else small_loop(IC<4>{}, acc, tiles, stores_behind);
+      int rows_left = 0;
       if constexpr (ADAPT)
-        if (cur.kb == 0) add_adapters(acc, cur, 0, wave * 64);
-      finish_segment(acc, IC<4>{});
+        if (cur.kb == 0) rows_left = add_adapters(acc, cur, 0, wave * 64);
+      finish_segment(acc, IC<4>{}, rows_left);
     }
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) {
