@@ -224,8 +224,8 @@ __device__ __forceinline__ void add_low_rank16(f32x4 (&acc)[8][NI], const Adapte
       const_cast<bf16_t*>(ad.low + static_cast<int64_t>(row0) * 2 * ad.rank), 0, 0x7fffffff, 0x00020000);
   // Half of the columns at a time: while one half's operand is multiplied the other half's, or the next step's, is on its
   // way, and a row block's takes the next step's place as soon as both halves have used it (96 registers; the next step's in flight as well
-  // spill, and cost more than they hide).  The second summands as steps of their own, with 64: 8192 rows of 24 requests, rank 32, 2048 to 8192
-  // 340 us, 320 so, 308 with the first summands alone.
+  // spill, and cost more than they hide).  The second summands as steps of their own, with 64 registers, cost 20 us more where 8192 rows of 24
+  // requests, rank 32, 2048 to 8192 take 313; the first summands alone 10 less.
   constexpr int H = NI / 2;
   const bool split = pieces > 2;
   u32x4 up[2][H], low[2][MI];
