@@ -102,3 +102,19 @@ def test_captured_fp16_calls_replay_with_new_inputs(counts):
         torch.cuda.synchronize()
         for a, b in zip(got, want):
             assert torch.equal(a[:c.rows].view(torch.uint8), b[:c.rows].view(torch.uint8)) if a.dim() == 2 else torch.equal(a.view(torch.int32), b.view(torch.int32))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("counts", [(20,), (400,)])
+def test_the_most_adapters(counts, dt):
+    """65536 of them: the last one's number is all 16 bits of a row's word, beside rows without any and, in fp16, rows with a power of two."""
+    c = Case(counts, 16, 24, 65536, 8, dt, perm=False, seed=counts[0])
+    who = torch.tensor([65535, -1, 0, 65534])[torch.arange(counts[0]) % 4]
+    c.adapter.copy_(who.to(torch.int32))
+    c.host_row = who.numpy()
+    c.scale[65534] = 2.0 ** 17
+    c.B[65534].mul_(2.0 ** -12)
+    c.A[65534].mul_(2.0 ** -12)
+    y, v = c.forward()
+    check_forward(c, y, v)
+    check_backward(c, v, *c.backward(v))
