@@ -699,7 +699,8 @@ inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) &
 
 int check_config(const moe_adapter_config* c) {
   if (c == nullptr) return MOE_ERR_NULL;
-  if (c->rows < 0 || c->rows > kMaxRows || c->K <= 0 || c->N <= 0 || (c->K & 7) || (c->N & 7) || c->K > kMaxColumns || c->N > kMaxColumns) return MOE_ERR_SHAPE;
+  if (c->rows < 0 || c->rows > kMaxRows) return MOE_ERR_SHAPE;
+  if (c->K <= 0 || c->N <= 0 || (c->K & 7) || (c->N & 7) || c->K > kMaxColumns || c->N > kMaxColumns) return MOE_ERR_SHAPE;
   if (c->n_exp < 1 || c->n_exp > kMaxExperts || c->n_adapters < 1 || c->n_adapters > kMaxPairs / c->n_exp) return MOE_ERR_SHAPE;
   if (c->rank < 8 || c->rank > kMaxRank || (c->rank & 7) || c->top_k < 1 || c->top_k > kMaxTopK) return MOE_ERR_SHAPE;
   if (!is_16bit(c->dtype)) return MOE_ERR_DTYPE;
@@ -896,7 +897,8 @@ int moe_adapter_forward(const moe_adapter_config* cfg, const void* x, const int3
   const size_t n_rows = cfg->rows, pairs = static_cast<size_t>(cfg->n_exp) * cfg->n_adapters, k = cfg->K, n = cfg->N, r = cfg->rank;
   const adapter::Memory memory[] = {{y, n_rows * n * 2}, {v, n_rows * r * 4}, {workspace, L.total}, {x, n_rows * k * 2},
                                     {offsets, (cfg->n_exp + 1) * size_t(4)}, {W, cfg->n_exp * n * k * 2}, {A, pairs * r * k * 2},
-                                    {B, pairs * n * r * 2}, {scale, cfg->n_adapters * size_t(4)}, {adapter, adapter::bytes_of_adapter(*cfg, perm)}, {perm, n_rows * 4}};
+                                    {B, pairs * n * r * 2}, {scale, cfg->n_adapters * size_t(4)},
+                                    {adapter, adapter::bytes_of_adapter(*cfg, perm)}, {perm, n_rows * 4}};
   if (adapter::overlapping(memory, 3)) return MOE_ERR_OVERLAP;
   hipStream_t s = static_cast<hipStream_t>(stream);
   unsigned char* ws = static_cast<unsigned char*>(workspace);

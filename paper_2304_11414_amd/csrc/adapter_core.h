@@ -203,10 +203,10 @@ __device__ __forceinline__ void hold(ACC& acc) {
 }
 
 // The persistent kernel's wavefront: 8 x NI blocks of 16x16x32 instructions, mine[mi] the adapter of row 16 mi + lane % 16 (-1: none,
-// or not a row of the tile), row0 and col0 its first row and column.  A step is up to 32 of one adapter's rank, of which both summands are at hand (up to
-// rank 16 both in one operand); blocks of 16
-// rows of which none has the adapter are passed over (8192 rows of 24 requests over 8 experts: four adapters per wavefront, each
-// in a third of its rows), so a step is little work and what it costs is the latency of its operands.
+// or not a row of the tile), row0 and col0 its first row and column.  A step is up to 32 of one adapter's rank, with both summands
+// (up to rank 16 in one operand); blocks of 16 rows of which none has the adapter are passed over (8192 rows of 24 requests over 8
+// experts: four adapters per wavefront, each in a third of its rows), so a step is little work and what it costs is the latency of
+// its operands.
 template <int DT, int NI>
 __device__ __forceinline__ void add_low_rank16(f32x4 (&acc)[8][NI], const AdapterRows& ad, const int (&mine)[8], int expert, int row0,
                                                int col0, int Nout) {

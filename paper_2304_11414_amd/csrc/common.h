@@ -148,7 +148,8 @@ struct Elem16<MOE_F16> {
 };
 inline bool is_16bit(int dtype) { return dtype == MOE_BF16 || dtype == MOE_F16; }
 
-// What a grouped product adds to its rows for their adapters (adapter_core.h); of_row[r]: the adapter of packed row r and a power of two, or -1 (adapter_of).
+// What a grouped product adds to its rows for their adapters (adapter_core.h); of_row[r]: the adapter of packed row r and a
+// power of two, or -1 (adapter_of).
 struct AdapterRows {
   const int32_t* of_row;
   const bf16_t* low;

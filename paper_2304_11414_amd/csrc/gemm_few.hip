@@ -34,7 +34,7 @@ constexpr int kLd = BN + 4;      // floats per row of partial sums in LDS
 // aux_rows[r] / aux_div of the matrix given as A.  2: packed row r belongs to assignment a = aux_rows[r] of
 // token a / aux_div; if it is that token's only kept pick here it is stored, times aux_w[a], as row `token`
 // of C, else unweighted as packed row r of C2.
-// ADAPT: the rows' adapters are added to the sums (a thread has four columns of one row: it reads four rows of `up` and one of `low`).
+// ADAPT: the rows' adapters are added to the sums (a thread has four columns of one row: it reads four rows of `up` and one of the float32 factor).
 template <bool GELU, int FUSE, int DT, bool ADAPT>
 __global__ __launch_bounds__(kThreads, 4) void grouped_gemm_few_rows_kernel(
     const bf16_t* __restrict__ A, const bf16_t* __restrict__ B, bf16_t* __restrict__ C,
