@@ -363,7 +363,8 @@ int moe_layer_forward_aux(const moe_config* cfg, const void* x, const void* Wg, 
  *   dA[a][i] = sum over its rows of t[r, :] x[r, :]^T              [n_adapters, n_exp, rank, K] float32
  *   dB[a][i] = sum over its rows of dy[r, :] (scale[a] v[r, :])^T   [n_adapters, n_exp, N, rank] float32
  * dA and dB are overwritten in full (zeros for a pair without rows) and hold float32 accuracy: t and v enter as 16-bit summands,
- * three with BF16, two with F16.  (K + N) * n_exp * n_adapters is at most 2^28 in the backward.
+ * three with BF16, two with F16 (22 bits, or 2^-38 of a pair's largest factor where that is more).  (K + N) * n_exp * n_adapters is
+ * at most 2^28 in the backward.
  * Sums have a fixed order: the same bits on every run.  Neither call allocates or, after moe_init, synchronises.
  * workspace: at least moe_adapter_workspace_bytes / moe_adapter_backward_workspace_bytes bytes (0 on an invalid config); calls
  * that share one must be ordered on one stream.  An output or the workspace that overlaps any other array of the call is refused

@@ -39,7 +39,7 @@ def test_forward(shape, dt):
 def test_backward(shape, dt):
     counts, N, K, n_a, rank, more = shape                       # (dx is the product from N to K)
     c = Case(counts, K, N, n_a, rank, dt, seed=K + N + 1, **{**more, "gelu": False})
-    v = torch.randn(c.rows + 5, rank, device="cuda")
+    v = torch.randn(c.rows + 5, rank, generator=torch.Generator().manual_seed(rank)).cuda()
     check_backward(c, v, *c.backward(v))
 
 
@@ -55,7 +55,7 @@ def test_cut_tiles_have_the_same_bits_however_they_are_handed_over(K, N, dt):
         case.scale = torch.tensor([1.0, 2.0 ** 17, 0.5, -1.0, 2.0 ** -18], device="cuda")
         case.B[1].mul_(2.0 ** -12)
         case.A[1].mul_(2.0 ** -5)
-    v = torch.randn(d.rows + 5, 24, device="cuda")
+    v = torch.randn(d.rows + 5, 24, generator=torch.Generator().manual_seed(K)).cuda()
     y, kept = c.forward()
     out = [y[:c.rows], kept[:c.rows], *(t[:d.rows] if t.dim() == 2 else t for t in d.backward(v))]
     check_forward(c, y, kept)

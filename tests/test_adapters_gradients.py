@@ -16,7 +16,7 @@ def test_an_infinite_factor_leaves_the_other_ones_their_accuracy(rank, dt):
     c = Case((90, 31), 128, 136, 3, rank, dt, mix="tokens", seed=rank)
     c.B[1, :, 5, 2] = float("inf")
     c.dy.mul_(2.0 ** -16)
-    v = torch.randn(c.rows + 5, rank, device="cuda") * 2.0 ** -16
+    v = (torch.randn(c.rows + 5, rank, generator=torch.Generator().manual_seed(rank)) * 2.0 ** -16).cuda()
     own = np.flatnonzero(c.host_row == 1)
     v[own[::3], 4] = float("inf")
     _, dA, dB = c.backward(v, dx=False)
@@ -39,7 +39,10 @@ def test_an_infinite_factor_leaves_the_other_ones_their_accuracy(rank, dt):
 def test_factors_keep_float32_accuracy(rank, counts, dt):
     """x and dy have one number per column, a power of two, so that an element of dA or dB is one factor times it, and the split into 16-bit
     summands all that it can lose: (2^-8)^3 of the factor (bf16, three summands) or (2^-11)^2 (fp16, two), and a rounding of 2^-24 per summand.
-    v has float32's 24 bits.  t = s (b1 + 2^-8 b2 + 2^-15 b3) for numbers b of B: three products and their float32 sum, so two roundings more."""
+    v has float32's 24 bits, a quarter of it far smaller than the rest.  t = s (b1 + 2^-8 b2 + 2^-15 b3) for numbers b of B: three products and
+    their float32 sum, so two roundings more.
+    fp16's smallest numbers are 2^-24 apart, so a second summand is off by 2^-25 at least: of factors that a power of two has brought to a
+    largest of 2^13 or more, so by 2^-38 of the pair's largest factor at most."""
     c = Case(counts, 264, 264, 3, rank, dt, mix="tokens", seed=rank + 100)
     c.scale = torch.tensor([0.5, -4.0, 1.0], device="cuda")
     g = torch.Generator().manual_seed(rank)
@@ -56,7 +59,9 @@ def test_factors_keep_float32_accuracy(rank, counts, dt):
         if with_t:
             z[:, :200] = 0
         c.x[:c.rows], c.dy[:c.rows] = x.to(DT[dt]).cuda(), z.to(DT[dt]).cuda()
-        v = torch.randn(c.rows + 5, rank, device="cuda")
+        v = torch.randn(c.rows + 5, rank, generator=g)
+        v[:, 1::4] *= 2.0 ** -18
+        v = v.cuda()
         _, dA, dB = c.backward(v, dx=False)
         X, dY, Bm, V, dA, dB = (f64(t) for t in (c.x, c.dy, c.B, v, dA, dB))
         bits = 2.0 ** -24 + 4 * 2.0 ** -24 if dt == "bf16" else 2.0 ** -22 + 3 * 2.0 ** -24
@@ -65,6 +70,8 @@ def test_factors_keep_float32_accuracy(rank, counts, dt):
                 continue
             if with_t:
                 t, S = c.s(a) * (dY[at] @ Bm[a, e]), abs(c.s(a)) * (np.abs(dY[at]) @ np.abs(Bm[a, e]))
-                close(dA[a, e], t.T @ X[at], (bits + 2 * 2.0 ** -24) * (S.T @ np.abs(X[at])), "dA")
+                floor = 2.0 ** -38 * np.abs(t).max(initial=0.0) * np.abs(X[at]).sum(0)[None] if dt == "f16" else 0.0
+                close(dA[a, e], t.T @ X[at], (bits + 2 * 2.0 ** -24) * (S.T @ np.abs(X[at])) + floor, "dA")
             else:
-                close(dB[a, e], c.s(a) * (dY[at].T @ V[at]), bits * abs(c.s(a)) * (np.abs(dY[at]).T @ np.abs(V[at])), "dB")
+                floor = 2.0 ** -38 * abs(c.s(a)) * np.abs(V[at]).max(initial=0.0) * np.abs(dY[at]).sum(0)[:, None] if dt == "f16" else 0.0
+                close(dB[a, e], c.s(a) * (dY[at].T @ V[at]), bits * abs(c.s(a)) * (np.abs(dY[at]).T @ np.abs(V[at])) + floor, "dB")
